@@ -346,6 +346,176 @@ int proxyattn_head_overlap(const proxyattn_problem* p, const void* q, const void
                            int32_t renormalize, float* scores, void* workspace,
                            size_t workspace_bytes, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Around the prefill: queries and keys normed and rotated before it, and a
+ * paged cache of keys and values after it (the paper's decode stays dense and
+ * reads every cached token).  The conventions above hold, with batches of
+ * sequences in place of one.
+ * ---------------------------------------------------------------------------
+ *
+ * Norm of each head and rotation by position.  A row is the d values of one
+ * head of one token.  With a weight w it is first normed,
+ *     y_j = x_j w_j / sqrt(mean(x^2) + norm_eps),
+ * and then its first rotary_dim values are rotated in pairs (a, b) by the
+ * angles of the token's position p,
+ *     z_a = y_a cos[p][j] - y_b sin[p][j],  z_b = y_b cos[p][j] + y_a sin[p][j],
+ * pair j being (j, j + rotary_dim/2), or (2j, 2j+1) when interleaved.  All of
+ * it is computed in 64 bits and rounded once to the problem's dtype.
+ *
+ *  rotary_dim: 0 (no rotation) or a multiple of 16 up to d.
+ *  cos, sin: device, fp32 [table_len][rotary_dim/2], 16-byte aligned (NULL
+ *      when rotary_dim is 0).
+ *  q_weight, k_weight: device, [d] in the problem's dtype, or NULL (no norm).
+ *  norm_eps: > 0 when there is a weight.
+ *  Output strides in elements; 0 selects the packed default (tok = H*d,
+ *      head = d).  Rows must start 16-byte aligned.
+ */
+typedef struct proxyattn_rotary {
+    uint32_t struct_size;  /* = sizeof(proxyattn_rotary) */
+    int32_t rotary_dim;
+    int32_t interleaved;   /* 0 or 1 */
+    int32_t table_len;     /* rows of cos and sin */
+    double norm_eps;
+    const float* cos;
+    const float* sin;
+    const void* q_weight;
+    const void* k_weight;
+    int64_t q_out_tok_stride, q_out_head_stride;
+    int64_t k_out_tok_stride, k_out_head_stride;
+} proxyattn_rotary;
+
+/*
+ * Norms and rotates Q and K of a prompt (what proxyattn_estimate and the
+ * prefill calls then take as q and k).
+ *  q, k: as for proxyattn_estimate (the problem's strides, so slices of one
+ *      projection will do); either may be NULL together with its output.
+ *  positions: device [N] int32 position of each token (values outside
+ *      [0, table_len) are clamped to it), or NULL: token t is at
+ *      first_position + t, which must stay below table_len.
+ *  q_out, k_out: [N][H][d] with the rotary's output strides.  An output may be
+ *      its own input when the strides are equal too; otherwise they must not
+ *      overlap.
+ * Of the problem only seq_len, the heads, head_dim, dtype and the q and kv
+ * strides matter, but all of it is validated.  No workspace.
+ */
+int proxyattn_norm_rotate(const proxyattn_problem* p, const proxyattn_rotary* r, const void* q,
+                          const void* k, const int32_t* positions, int32_t first_position,
+                          void* q_out, void* k_out, void* stream);
+
+/* What the pages of a cache hold. */
+#define PROXYATTN_CACHE_SAME 0 /* the problem's dtype */
+#define PROXYATTN_CACHE_FP4 1  /* 4-bit values with one scale for 32 of them */
+
+/*
+ * A paged cache of the keys and values of one layer, and one call's batch.
+ *
+ * Pages.  A page holds page_size consecutive tokens ("slots") of one sequence.
+ * k_pages and v_pages, PROXYATTN_CACHE_SAME: [num_pages][Hkv][page_size][d] in
+ * the problem's dtype.  PROXYATTN_CACHE_FP4: [num_pages][Hkv][page_size][d/2]
+ * bytes, two values a byte, the even one in the low half, beside k_scales and
+ * v_scales [num_pages][Hkv][d/32][page_size] bytes: a value is
+ * (-1)^s {0, 1/2, 1, 3/2, 2, 3, 4, 6}[c] 2^(scale - 127) with s the top and c
+ * the low three bits of its half byte (E2M1 with an E8M0 scale for each 32
+ * values along d), scale from 17 to 252.  Appending picks the smallest scale, from 2^-110 to 2^125,
+ * of which no value of the 32 is more than 7 times, and the nearest value (ties to
+ * the even code, above 6 to 6), from what the problem's dtype would hold.
+ * All four: device, 16-byte aligned, proxyattn_cache_size bytes; no scales
+ * with PROXYATTN_CACHE_SAME.
+ *
+ * Sequences.  page_table [B][table_width] int32: page of tokens
+ * j*page_size .. of sequence b.  Entries that no token of the sequence needs
+ * are not read.  seq_lens [B] int32: tokens of each sequence, the call's own
+ * among them.  The call's tokens are packed: rows new_start[b] ..
+ * new_start[b+1]-1 of its q, k, v and out arrays are the last tokens of
+ * sequence b, in order (new_start [B+1] int32, not decreasing), the last one at
+ * position seq_lens[b]-1.  new_start NULL: one token a sequence, row b.
+ * Rows from new_start[B] on are neither read nor written (padded batches).
+ * All three: device, 4-byte aligned.  The library sees them only inside
+ * kernels, so bad values cannot be refused; they never make a kernel leave
+ * its arrays: lengths count up to max_len, new tokens of a sequence up to
+ * max_new, a row at a position below 0 is a token of no sequence; a page outside
+ * [0, num_pages) takes no token when appending, gives none when reading back and is
+ * clamped in the attention.
+ *
+ * Two sequences may share pages (a common beginning) as long as no call
+ * appends to a shared one; tokens appended to one slot by one call, which only
+ * such a table gives, leave either.
+ *
+ * Supported: d in {64, 128}; page_size in {16, 32, 64, 128, 256}; B <= 4096;
+ * Hq <= 4096, Hq % Hkv == 0; max_len <= table_width * page_size <= 2^30.
+ */
+typedef struct proxyattn_cache {
+    uint32_t struct_size;   /* = sizeof(proxyattn_cache) */
+    int32_t num_seqs;       /* B >= 0 */
+    int32_t num_tokens;     /* rows of the call's token arrays (>= B when new_start is NULL) */
+    int32_t max_new;        /* most new tokens of one sequence, >= 1 */
+    int32_t max_len;        /* most tokens of one sequence, >= 1 */
+    int32_t num_q_heads;
+    int32_t num_kv_heads;
+    int32_t head_dim;
+    int32_t page_size;
+    int32_t num_pages;      /* >= 1 */
+    int32_t table_width;    /* row length of page_table */
+    int32_t dtype;          /* of q, k, v and out: PROXYATTN_BF16 or PROXYATTN_F32 */
+    int32_t cache_type;     /* PROXYATTN_CACHE_SAME or PROXYATTN_CACHE_FP4 */
+    float softmax_scale;    /* <= 0 selects 1/sqrt(d) */
+    /* token arrays [num_tokens][H][d]: strides in elements, 0 = packed */
+    int64_t q_tok_stride, q_head_stride;
+    int64_t kv_tok_stride, kv_head_stride; /* shared by K and V */
+    int64_t o_tok_stride, o_head_stride;
+} proxyattn_cache;
+
+/* Bytes of k_pages (as many of v_pages) and of k_scales (as many of v_scales;
+ * 0 with PROXYATTN_CACHE_SAME). */
+int proxyattn_cache_size(const proxyattn_cache* c, size_t* page_bytes, size_t* scale_bytes);
+
+/*
+ * Appends the call's keys and values to the pages, the keys normed and rotated
+ * by their positions on the way (r NULL: as they are), and norms and rotates
+ * the call's queries into q_out in the same launch (q and q_out NULL: keys and
+ * values alone; r NULL: they must be).
+ *  q [T][Hq][d], k, v [T][Hkv][d]: the cache's strides.  q_out: the rotary's
+ *      q_out strides (its k_out strides are not used); it may be q.
+ *  table_len >= max_len is required where rotary_dim is not 0.
+ * No workspace.
+ */
+int proxyattn_cache_append(const proxyattn_cache* c, const proxyattn_rotary* r, const void* q,
+                           const void* k, const void* v, void* q_out, const int32_t* page_table,
+                           const int32_t* seq_lens, const int32_t* new_start, void* k_pages,
+                           void* v_pages, void* k_scales, void* v_scales, void* stream);
+
+/*
+ * Reads the last tokens of each sequence back from the pages, in the problem's
+ * dtype (exact for 4-bit values): rows new_start[b] .. new_start[b+1]-1 of
+ * k_out and v_out [T][Hkv][d] (the cache's kv strides) get the last
+ * new_start[b+1] - new_start[b] tokens of sequence b; max_new does not bound
+ * them.  k_out or v_out may be NULL.  No workspace.
+ */
+int proxyattn_cache_read(const proxyattn_cache* c, const int32_t* page_table,
+                         const int32_t* seq_lens, const int32_t* new_start, const void* k_pages,
+                         const void* v_pages, const void* k_scales, const void* v_scales,
+                         void* k_out, void* v_out, void* stream);
+
+/*
+ * Attention of the call's tokens over the cache (their own keys and values
+ * appended before): the token at position p of sequence b sees cached tokens
+ * 0 .. p,
+ *     out[t][i] = softmax_u(c <q_t, k_u>) v_u,  lse[i][t] = log sum_u exp(c <q_t, k_u>).
+ *  q: [T][Hq][d]; out: [T][Hq][d]; the cache's q and o strides.
+ *  lse: [Hq][T] fp32, or NULL.
+ *  workspace: at least proxyattn_cache_workspace_size bytes, 16-byte aligned;
+ *      nothing in it outlasts the call.
+ * Made for few new tokens a sequence: every 16 to 64 (token, head) rows of a KV
+ * head read its cache once.  A whole prompt is the prefill calls' work.
+ */
+int proxyattn_cache_workspace_size(const proxyattn_cache* c, size_t* bytes);
+int proxyattn_cache_attention(const proxyattn_cache* c, const void* q, const int32_t* page_table,
+                              const int32_t* seq_lens, const int32_t* new_start,
+                              const void* k_pages, const void* v_pages, const void* k_scales,
+                              const void* v_scales, void* out, float* lse, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
 /* Static text for a return code. */
 const char* proxyattn_error_string(int code);
 

@@ -10,14 +10,14 @@
 #include <string.h>
 
 #include "proxyattn.h"
+#include "errors.h"
 #include "internal.h"
 
 namespace pa {
 
 static thread_local char g_last_error[512] = "";
 
-static int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
-static int fail(int code, const char* fmt, ...) {
+int fail(int code, const char* fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
     vsnprintf(g_last_error, sizeof(g_last_error), fmt, ap);
@@ -25,16 +25,17 @@ static int fail(int code, const char* fmt, ...) {
     return code;
 }
 
-static int hip_fail(hipError_t e, const char* where) {
+int hip_fail(hipError_t e, const char* where) {
     return fail(PROXYATTN_E_HIP, "%s: %s", where, hipGetErrorString(e));
 }
+
+void clear_error() { g_last_error[0] = 0; }
 
 static size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 
 static bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
-// Validates the descriptor and resolves it into a Shape.
-static int resolve(const proxyattn_problem* p, Shape* sh) {
+int resolve(const proxyattn_problem* p, Shape* sh) {
     if (!p) return fail(PROXYATTN_E_INVALID, "problem is NULL");
     if (p->struct_size != sizeof(proxyattn_problem))
         return fail(PROXYATTN_E_INVALID, "struct_size %u != %zu", p->struct_size,
@@ -217,23 +218,11 @@ static int check_ws(const Shape& sh, const void* ws, size_t bytes, WsLayout* L) 
     return PROXYATTN_OK;
 }
 
-static int check_ptr(const void* p, const char* name) {
+int check_ptr(const void* p, const char* name) {
     if (!p) return fail(PROXYATTN_E_INVALID, "%s is NULL", name);
     if (!aligned16(p)) return fail(PROXYATTN_E_INVALID, "%s not 16-byte aligned", name);
     return PROXYATTN_OK;
 }
-
-#define PA_TRY(expr)                         \
-    do {                                     \
-        const int rc_ = (expr);              \
-        if (rc_ != PROXYATTN_OK) return rc_; \
-    } while (0)
-
-#define PA_LAUNCH(expr, where)                        \
-    do {                                              \
-        const hipError_t e_ = (expr);                 \
-        if (e_ != hipSuccess) return hip_fail(e_, where); \
-    } while (0)
 
 }  // namespace pa
 

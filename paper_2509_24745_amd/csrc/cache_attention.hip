@@ -1,0 +1,761 @@
+// Attention of a batch's newest tokens over the paged cache.
+//
+// The rows of a (sequence, KV head) are its new tokens' query heads, 16 NR of
+// them to a workgroup; a wave walks its share of the cached keys in steps of
+// 16 KT:
+//   S^T = K Q^T    (16x16 MFMA, keys by rows)
+//   P^T = exp2(S^T - reference), the sums and the largest score beside it
+//   O^T += V^T P^T (16x16 MFMA, values of a head by rows)
+// Lane l holds row n = l % 16 of every tile (g = l / 16).  S^T leaves it the
+// scores of keys KT (4 g + r) + t of the step (tile t < KT, r < 4): 4 KT
+// consecutive keys, and just those that the second product wants from it, so
+// P never leaves its lane.  K comes as one 16-byte piece of a key per lane and
+// product, V as the 4 KT keys of the lane's group, D/16 values of each, and both go from
+// memory to registers: no other wave wants them.  What the MFMAs take for a
+// key's index or a value's is free as long as both operands agree, which is
+// what picks the orders here (see Compute).
+//
+// Work is dealt flat: every (sequence, KV head, row tile) is a run of units of
+// 64 KT keys, all runs lie end to end, and workgroup w of W takes the w-th
+// equal part, whatever the lengths are.  A run cut between workgroups leaves
+// partial rows (reference, sum, output) in the workspace, added up in order by
+// a second launch.
+//
+// Bound: the cache's bytes.  A key and its value take 4 D bytes in bf16 and
+// 17/16 D in 4 bits, for 4 D products a row; at 16 rows that is 16 and 60
+// products a byte, where the card's rates balance at 250.
+#include <algorithm>
+
+#include "cache.h"
+#include "cache_device.h"
+#include "common.h"
+#include "proxyattn.h"
+
+namespace pa {
+
+constexpr int kAttnThreads = 256;   // 4 waves
+// Below any score that a finite row gives: the reference before the first key.
+constexpr float kNoScore = -1e30f;
+// Scores above the reference by this much (log2) move it: the sums grow by
+// 2^kSlack at most.
+constexpr float kSlack = 8.f;
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// 16-key tiles of a step: 64 keys in 4 bits, 32 otherwise.
+template <bool FP4> constexpr int key_tiles() { return FP4 ? 4 : 2; }
+
+// A sequence of the batch as the header reads its arrays.
+struct Seq {
+    int len, row, fresh;   // cached tokens, first row, new tokens
+};
+__device__ __forceinline__ Seq seq_at(const CacheShape& s, const int* lens, const int* starts,
+                                      int b) {
+    Seq q;
+    q.len = min(max(lens[b], 0), s.max_len);
+    q.row = b;
+    q.fresh = 1;
+    if (starts) {
+        q.row = min(max(starts[b], 0), s.t);
+        q.fresh = min(max(min(starts[b + 1], s.t) - q.row, 0), s.max_new);
+    }
+    return q;
+}
+
+// Row tiles of a KV head and units of a row tile.
+template <int ROWS, int UNIT> struct Runs {
+    int tiles, units;
+    __device__ __forceinline__ Runs(const CacheShape& s, const Seq& q)
+        : tiles((q.fresh * s.rep + ROWS - 1) / ROWS), units(max(1, (q.len + UNIT - 1) / UNIT)) {}
+};
+
+__device__ __forceinline__ int wave_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Which sequence a flat unit lies in, its first unit, and the number of all
+// units.  A block of 256 threads; plan (not NULL): every sequence's first unit
+// is left there, the total behind them.
+template <int ROWS, int UNIT>
+__device__ __forceinline__ void find_unit(const CacheShape& s, const int* lens, const int* starts,
+                                          int* plan, int64_t groups, int group, int* total,
+                                          int* per, int* b_out, int* base_out) {
+    __shared__ int wave_sum_[4];
+    __shared__ int found[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int chunk = (s.b + kAttnThreads - 1) / kAttnThreads;
+    const int b0 = tid * chunk, b1 = min(b0 + chunk, s.b);
+    auto count = [&](int b) {
+        const Runs<ROWS, UNIT> r(s, seq_at(s, lens, starts, b));
+        return s.hkv * r.tiles * r.units;
+    };
+    int mine = 0;
+    for (int b = b0; b < b1; ++b) mine += count(b);
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const int x = __shfl_up(incl, o);
+        if (lane >= o) incl += x;
+    }
+    if (lane == 63) wave_sum_[wave] = incl;
+    __syncthreads();
+    int before = incl - mine, all = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (w < wave) before += wave_sum_[w];
+        all += wave_sum_[w];
+    }
+    const int each = (int)((all + groups - 1) / groups);
+    const int64_t want = (int64_t)each * group;
+    if ((want >= before && want < before + mine) || (plan && mine)) {
+        int at = before;
+        for (int b = b0; b < b1; ++b) {
+            const int n = count(b);
+            if (plan) plan[b] = at;
+            if (want >= at && want < at + n) {
+                found[0] = b;
+                found[1] = at;
+            }
+            at += n;
+        }
+    } else if (plan) {
+        for (int b = b0; b < b1; ++b) plan[b] = before;
+    }
+    if (plan && tid == 0) plan[s.b] = all;
+    __syncthreads();
+    *total = all;
+    *per = each;
+    *b_out = want < all ? wave_uniform(found[0]) : 0;
+    *base_out = want < all ? wave_uniform(found[1]) : 0;
+}
+
+// ---------------------------------------------------------------------------
+// K and V of a step, from memory to registers
+// ---------------------------------------------------------------------------
+template <typename T, bool FP4, int D> struct KeyStep;
+
+// The problem's own type.  Chunk i of a key is its values 16 B of which lane
+// group g holds: for bf16 8 values 32 i + 8 g, for fp32 4 values 16 i + 4 g.
+template <typename T, int D> struct KeyStep<T, false, D> {
+    static constexpr int KT = 2, N = 16 / sizeof(T);
+    static constexpr int KC = D / 4 / N;              // 16-byte pieces of a key for a lane
+    static constexpr int VW = D / 16 * sizeof(T) / 4; // words of a value row for a lane
+    u32x4 k[KT][KC];
+    uint32_t v[4 * KT][VW];
+
+    __device__ __forceinline__ void load(const CacheShape& s, const PagePtrs& pg, int kpage,
+                                         int vpage, int head, int kpos, int vpos, int lane) {
+        const int g = lane >> 4, m = lane & 15, mask = (1 << s.page_shift) - 1;
+        const T* kp = (const T*)pg.k +
+                      ((((int64_t)kpage * s.hkv + head) << s.page_shift) + (kpos & mask)) * D + N * g;
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int i = 0; i < KC; ++i)
+                k[t][i] = *reinterpret_cast<const u32x4*>(kp + t * D + 4 * N * i);
+        const T* vp = (const T*)pg.v +
+                      ((((int64_t)vpage * s.hkv + head) << s.page_shift) + (vpos & mask)) * D +
+                      D / 16 * m;
+#pragma unroll
+        for (int x = 0; x < 4 * KT; ++x) {
+            if constexpr (VW % 4 == 0) {
+#pragma unroll
+                for (int i = 0; i < VW; i += 4) {
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(vp + x * D + i * 4 / sizeof(T));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[x][i + j] = w[j];
+                }
+            } else {
+                const u32x2 w = *reinterpret_cast<const u32x2*>(vp + x * D);
+                v[x][0] = w[0];
+                v[x][1] = w[1];
+            }
+        }
+    }
+    // Values from key `from` of the lane's on are none: a probability of 0 times
+    // what an unwritten slot holds has to be 0.
+    __device__ __forceinline__ void drop_values(int from) {
+#pragma unroll
+        for (int x = 0; x < 4 * KT; ++x)
+#pragma unroll
+            for (int i = 0; i < VW; ++i) v[x][i] = x < from ? v[x][i] : 0u;
+    }
+};
+
+// 4 bits.  A lane holds the D/4 values (D/4) g .. of each of its keys, D/16 of
+// each of its values, and their scales.
+template <typename T, int D> struct KeyStep<T, true, D> {
+    static constexpr int KT = 4;
+    static constexpr int KC = D / 32;   // words of a key for a lane
+    uint32_t k[KT][KC];
+    uint32_t ks;        // scales of the lane's KT keys, a byte each
+    uint32_t v[4 * KT]; // D = 64: the low half
+    u32x4 vs;           // scales of the lane's 16 values
+
+    __device__ __forceinline__ void load(const CacheShape& s, const PagePtrs& pg, int kpage,
+                                         int vpage, int head, int kpos, int vpos, int lane) {
+        const int g = lane >> 4, m = lane & 15, mask = (1 << s.page_shift) - 1;
+        const int64_t kh = (int64_t)kpage * s.hkv + head, vh = (int64_t)vpage * s.hkv + head;
+        const uint8_t* kp = (const uint8_t*)pg.k +
+                            ((kh << s.page_shift) + (kpos & mask)) * (D / 2) + D / 8 * g;
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+            if constexpr (KC == 4) {
+                const u32x4 w = *reinterpret_cast<const u32x4*>(kp + t * (D / 2));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) k[t][j] = w[j];
+            } else {
+                const u32x2 w = *reinterpret_cast<const u32x2*>(kp + t * (D / 2));
+                k[t][0] = w[0];
+                k[t][1] = w[1];
+            }
+        }
+        ks = *reinterpret_cast<const uint32_t*>(
+            (const uint8_t*)pg.ks +
+            ((kh * (D / 32) + g * (D / 4) / 32) << s.page_shift) + (kpos & mask));
+        const uint8_t* vp = (const uint8_t*)pg.v +
+                            ((vh << s.page_shift) + (vpos & mask)) * (D / 2) + D / 32 * m;
+#pragma unroll
+        for (int x = 0; x < 4 * KT; ++x) {
+            if constexpr (D == 128)
+                v[x] = *reinterpret_cast<const uint32_t*>(vp + x * (D / 2));
+            else
+                v[x] = *reinterpret_cast<const uint16_t*>(vp + x * (D / 2));
+        }
+        vs = *reinterpret_cast<const u32x4*>(
+            (const uint8_t*)pg.vs +
+            ((vh * (D / 32) + m * (D / 16) / 32) << s.page_shift) + (vpos & mask));
+    }
+    // A scale of an unwritten slot may be no number; 0 times a value is 0.
+    __device__ __forceinline__ void drop_values(int from) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int keep = min(max(from - 4 * j, 0), 4);
+            vs[j] = keep == 4 ? vs[j] : vs[j] & ((1u << (8 * keep)) - 1u);
+        }
+    }
+    __device__ __forceinline__ float kscale(int t) const {
+        return __uint_as_float((ks >> (8 * t) & 255u) << 23);
+    }
+    __device__ __forceinline__ float vscale(int x) const {
+        return __uint_as_float((vs[x / 4] >> (8 * (x % 4)) & 255u) << 23);
+    }
+};
+
+// ---------------------------------------------------------------------------
+// products
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ f32x4 mma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma16(float a, float b, const f32x4& c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t pack_rne(float lo, float hi) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const f32x2 x = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+}
+__device__ __forceinline__ uint32_t fp4_pair_bf16(uint32_t w, float scale, int byte) {
+    switch (byte) {   // the byte is an immediate
+        case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+        case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+        case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+        default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+    }
+}
+__device__ __forceinline__ bf16x8 as_frag(const u32x4& w) { return __builtin_bit_cast(bf16x8, w); }
+
+// The rows' side of the products for NR tiles of 16 rows, and a step.
+template <typename T, bool FP4, int D, int NR> struct Rows;
+
+// bf16: MFMAs of 32 products.  For the scores, product i of lane group g takes
+// the values that chunk i of KeyStep holds; for the outputs, product (u, i)
+// takes the keys of tiles 2 u and 2 u + 1 and value D/16 m + i of row m, and two of
+// them: the probabilities as a bf16 and the bf16 of what that rounds off, so
+// that the output's own rounding is the only one that shows.  The second products
+// wait beside the loads.
+template <bool FP4, int D, int NR> struct Rows<bf16, FP4, D, NR> {
+    typedef KeyStep<bf16, FP4, D> Keys;
+    static constexpr int KT = Keys::KT, QC = D / 32, OC = D / 16;
+    bf16x8 q[NR][QC];
+    f32x4 o[NR][OC];
+
+    __device__ __forceinline__ void load_query(int nr, const bf16* row, int g) {
+#pragma unroll
+        for (int i = 0; i < QC; ++i) {
+            u32x4 w = zero_u32x4();
+            if (row) w = *reinterpret_cast<const u32x4*>(row + (FP4 ? D / 4 * g + 8 * i
+                                                                    : 32 * i + 8 * g));
+            q[nr][i] = as_frag(w);
+        }
+    }
+    __device__ __forceinline__ void scores(const Keys& ks, f32x4 (&x)[NR][KT]) const {
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+            bf16x8 kf[QC];
+#pragma unroll
+            for (int i = 0; i < QC; ++i) {
+                if constexpr (FP4) {
+                    u32x4 w;
+                    const float sc = ks.kscale(t);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = fp4_pair_bf16(ks.k[t][i], sc, j);
+                    kf[i] = as_frag(w);
+                } else {
+                    kf[i] = as_frag(ks.k[t][i]);
+                }
+            }
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) {
+                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < QC; ++i) acc = mma16(kf[i], q[nr][i], acc);
+                x[nr][t] = acc;
+            }
+        }
+    }
+    __device__ __forceinline__ void outputs(const Keys& ks, const f32x4 (&p)[NR][KT]) {
+#pragma unroll
+        for (int u = 0; u < KT / 2; ++u) {
+            bf16x8 hi[NR], lo[NR];
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) {
+                u32x4 h, l;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const float a = p[nr][2 * u + w / 2][2 * (w % 2)];
+                    const float b = p[nr][2 * u + w / 2][2 * (w % 2) + 1];
+                    h[w] = pack_rne(a, b);
+                    l[w] = pack_rne(a - __uint_as_float(h[w] << 16),
+                                    b - __uint_as_float(h[w] & 0xffff0000u));
+                }
+                hi[nr] = as_frag(h);
+                lo[nr] = as_frag(l);
+            }
+            // slots 2 w, 2 w + 1 of the fragment: keys KT r + 2 u + w / 2, r = 2 (w % 2) and the next
+#pragma unroll
+            for (int c = 0; c < OC / 2; ++c) {   // values 2 c and 2 c + 1 of the lane's
+                u32x4 even, odd;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int x0 = KT * 2 * (w % 2) + 2 * u + w / 2, x1 = x0 + KT;
+                    uint32_t a, b;
+                    if constexpr (FP4) {
+                        a = fp4_pair_bf16(ks.v[x0], ks.vscale(x0), c);
+                        b = fp4_pair_bf16(ks.v[x1], ks.vscale(x1), c);
+                    } else {
+                        a = ks.v[x0][c];
+                        b = ks.v[x1][c];
+                    }
+                    even[w] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+                    odd[w] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+                }
+#pragma unroll
+                for (int nr = 0; nr < NR; ++nr) {
+                    o[nr][2 * c] = mma16(as_frag(even), hi[nr], o[nr][2 * c]);
+                    o[nr][2 * c + 1] = mma16(as_frag(odd), hi[nr], o[nr][2 * c + 1]);
+                    o[nr][2 * c] = mma16(as_frag(even), lo[nr], o[nr][2 * c]);
+                    o[nr][2 * c + 1] = mma16(as_frag(odd), lo[nr], o[nr][2 * c + 1]);
+                }
+            }
+        }
+    }
+};
+
+// fp32: MFMAs of 4 products, one value of each lane group, exact as fp32
+// products are.  Their rate, 1/16 of bf16's, still outruns the cache's bytes
+// four times.
+template <bool FP4, int D, int NR> struct Rows<float, FP4, D, NR> {
+    typedef KeyStep<float, FP4, D> Keys;
+    static constexpr int KT = Keys::KT, QC = D / 4, OC = D / 16;
+    float q[NR][QC];
+    f32x4 o[NR][OC];
+
+    __device__ __forceinline__ void load_query(int nr, const float* row, int g) {
+#pragma unroll
+        for (int i = 0; i < QC / 4; ++i) {
+            f32x4 w = {0.f, 0.f, 0.f, 0.f};
+            if (row) w = *reinterpret_cast<const f32x4*>(row + (FP4 ? D / 4 * g + 4 * i
+                                                                    : 16 * i + 4 * g));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[nr][4 * i + j] = w[j];
+        }
+    }
+    __device__ __forceinline__ void scores(const Keys& ks, f32x4 (&x)[NR][KT]) const {
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+            f32x4 acc[NR];
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) acc[nr] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < QC / 8; ++i) {
+                float kf[8];
+                if constexpr (FP4) {
+                    fp4_values(ks.k[t][i], ks.kscale(t), kf);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) kf[j] = __uint_as_float(ks.k[t][2 * i + j / 4][j % 4]);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int nr = 0; nr < NR; ++nr) acc[nr] = mma16(kf[j], q[nr][8 * i + j], acc[nr]);
+            }
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) x[nr][t] = acc[nr];
+        }
+    }
+    __device__ __forceinline__ void outputs(const Keys& ks, const f32x4 (&p)[NR][KT]) {
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int x = KT * r + t;
+                float vf[OC];
+                if constexpr (FP4) {
+                    float z[8];
+                    fp4_values(ks.v[x], ks.vscale(x), z);
+#pragma unroll
+                    for (int i = 0; i < OC; ++i) vf[i] = z[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < OC; ++i) vf[i] = __uint_as_float(ks.v[x][i]);
+                }
+#pragma unroll
+                for (int i = 0; i < OC; ++i)
+#pragma unroll
+                    for (int nr = 0; nr < NR; ++nr) o[nr][i] = mma16(vf[i], p[nr][t][r], o[nr][i]);
+            }
+    }
+};
+
+// Over the four lane groups, which hold the same rows.
+__device__ __forceinline__ float groups_max(float x) {
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return halves_max(x);
+}
+__device__ __forceinline__ float groups_sum(float x) {
+    x += __shfl_xor(x, 16);
+    return halves_sum(x);
+}
+
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[8]);
+template <> __device__ __forceinline__ void store8<bf16>(bf16* p, const float (&x)[8]) {
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = pack_rne(x[2 * j], x[2 * j + 1]);
+    *reinterpret_cast<u32x4*>(p) = w;
+}
+template <> __device__ __forceinline__ void store8<float>(float* p, const float (&x)[8]) {
+    *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+
+template <typename T, bool FP4, int D, int NR>
+__global__ __launch_bounds__(kAttnThreads) void cache_attn_kernel(
+    CacheShape s, const T* qp, const int* table, const int* lens, const int* starts, PagePtrs pg,
+    T* out, float* lse, int* plan, float2* stat, float* part) {
+    typedef KeyStep<T, FP4, D> Keys;
+    constexpr int KT = Keys::KT, SK = 16 * KT, UNIT = 4 * SK, ROWS = 16 * NR, OC = D / 16;
+    constexpr int LINE = D + 4;   // a row's outputs in LDS, padded by a bank group
+    __shared__ __align__(16) float merge[4][16][LINE];
+    __shared__ float2 wstat[4][ROWS];
+    const int lane = threadIdx.x & 63, wave = wave_uniform(threadIdx.x >> 6);
+    const int g = lane >> 4, n = lane & 15;
+    const int group = blockIdx.x;
+
+    int total, per, b, base;
+    find_unit<ROWS, UNIT>(s, lens, starts, group == 0 ? plan : nullptr, gridDim.x, group, &total,
+                          &per, &b, &base);
+    int64_t f = (int64_t)per * group;
+    const int64_t fend = min(f + per, (int64_t)total);
+    bool first = true;
+    while (f < fend) {
+        Seq sq = seq_at(s, lens, starts, b);
+        sq.len = wave_uniform(sq.len);
+        sq.row = wave_uniform(sq.row);
+        sq.fresh = wave_uniform(sq.fresh);
+        const Runs<ROWS, UNIT> run(s, sq);
+        if (f >= (int64_t)base + (int64_t)s.hkv * run.tiles * run.units) {   // on to the next
+            base += s.hkv * run.tiles * run.units;
+            ++b;
+            continue;
+        }
+        const int at = (int)(f - base), item = at / run.units, u0 = at - item * run.units;
+        const int u1 = (int)min((int64_t)run.units, u0 + (fend - f));
+        const int head = item / run.tiles, row0 = (item - head * run.tiles) * ROWS;
+        f += u1 - u0;
+
+        // rows: (new token, query head of the KV head); row n of tile nr sees keys up to limit
+        const int rows = sq.fresh * s.rep, newest = sq.len - sq.fresh;
+        Rows<T, FP4, D, NR> r;
+        int limit[NR];
+        float ref[NR], sum[NR];
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr) {
+            const int row = row0 + 16 * nr + n;
+            const int j = row / s.rep;
+            const T* q = nullptr;
+            limit[nr] = sq.len - 1;
+            if (row < rows) {
+                limit[nr] = newest + j;
+                q = qp + (int64_t)(sq.row + j) * s.q_tok +
+                    (int64_t)(head * s.rep + row - j * s.rep) * s.q_head;
+            }
+            r.load_query(nr, q, g);
+            ref[nr] = kNoScore;
+            sum[nr] = 0.f;
+#pragma unroll
+            for (int i = 0; i < OC; ++i) r.o[nr][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        const int all_see = newest + row0 / s.rep;   // keys up to here: every row
+        const int some_see = newest + (min(row0 + ROWS, rows) - 1) / s.rep;
+        const int key0 = u0 * UNIT, key1 = min(u1 * UNIT, some_see + 1);
+
+        // page of a step's keys for this lane, inside the sequence
+        const int* pages = table + (int64_t)b * s.width;
+        const int klast = (sq.len - 1) & ~(KT - 1), vlast = (sq.len - 1) & ~(4 * KT - 1);
+        auto kpos = [&](int s0) { return min(s0 + KT * n, klast); };
+        auto vpos = [&](int s0) { return min(s0 + 4 * KT * g, vlast); };
+        auto page = [&](int pos) { return pages[pos >> s.page_shift]; };
+        auto clamp_page = [&](int p) { return min(max(p, 0), s.num_pages - 1); };
+
+        auto step = [&](Keys& ks, int s0) {
+            f32x4 x[NR][KT];
+            r.scores(ks, x);
+            if (s0 + SK > sq.len) ks.drop_values(sq.len - (s0 + 4 * KT * g));
+            const bool ends = s0 + SK - 1 > all_see;
+#pragma unroll
+            for (int nr = 0; nr < NR; ++nr) {
+                float top = kNegInf;
+#pragma unroll
+                for (int t = 0; t < KT; ++t)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float y = x[nr][t][c] * s.scale2;
+                        if (ends && s0 + KT * (4 * g + c) + t > limit[nr]) y = kNegInf;
+                        x[nr][t][c] = y;
+                        top = fmaxf(top, y);
+                    }
+                if (__any(top > ref[nr] + kSlack)) {
+                    const float next = fmaxf(ref[nr], groups_max(top));
+                    const float shrink = fast_exp2(ref[nr] - next);
+                    ref[nr] = next;
+                    sum[nr] *= shrink;
+#pragma unroll
+                    for (int i = 0; i < OC; ++i) r.o[nr][i] *= shrink;
+                }
+#pragma unroll
+                for (int t = 0; t < KT; ++t)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const float p = fast_exp2(x[nr][t][c] - ref[nr]);
+                        x[nr][t][c] = p;
+                        sum[nr] += p;
+                    }
+            }
+            r.outputs(ks, x);
+        };
+
+        // Steps key0 + SK (wave + 4 j).  Two register sets: one step's loads
+        // run beside the other's products; pages are looked up a step further
+        // ahead (their loads come first, so that waiting for them waits for
+        // nothing else).
+        int s0 = key0 + SK * wave;
+        if (s0 < key1) {
+            Keys ka, kb;
+            int kp = page(kpos(s0)), vp = page(vpos(s0));
+            auto fetch = [&](Keys& ks, int at_key) {   // at_key's pages are in kp, vp
+                const int kc = clamp_page(kp), vc = clamp_page(vp);
+                const int ahead = at_key + 4 * SK;
+                kp = page(kpos(ahead));
+                vp = page(vpos(ahead));
+                ks.load(s, pg, kc, vc, head, kpos(at_key), vpos(at_key), lane);
+            };
+            fetch(ka, s0);
+            while (true) {
+                const int s1 = s0 + 4 * SK, s2 = s1 + 4 * SK;
+                if (s1 < key1) fetch(kb, s1);
+                step(ka, s0);
+                if (s1 >= key1) break;
+                if (s2 < key1) fetch(ka, s2);
+                step(kb, s1);
+                if (s2 >= key1) break;
+                s0 = s2;
+            }
+        }
+
+        // the four waves' rows together
+        const bool whole = u0 == 0 && u1 == run.units;
+        const int slot = 2 * group + (first ? 0 : 1);
+        first = false;
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr) {
+            sum[nr] = groups_sum(sum[nr]);
+            if (g == 0) wstat[wave][16 * nr + n] = float2{ref[nr], sum[nr]};
+        }
+        __syncthreads();
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr) {
+            float top = kNoScore;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) top = fmaxf(top, wstat[w][16 * nr + n].x);
+            const float shrink = fast_exp2(ref[nr] - top);
+#pragma unroll
+            for (int c = 0; c < 4; ++c)   // values OC (4 g + c) ..
+#pragma unroll
+                for (int i = 0; i < OC; i += 4)
+                    *reinterpret_cast<f32x4*>(&merge[wave][n][OC * (4 * g + c) + i]) =
+                        f32x4{r.o[nr][i][c], r.o[nr][i + 1][c], r.o[nr][i + 2][c],
+                              r.o[nr][i + 3][c]} * shrink;
+            __syncthreads();
+            // 16 rows of D/8 pieces of 8 values
+            const int piece = threadIdx.x % (D / 8);
+            for (int line = threadIdx.x / (D / 8); line < 16; line += kAttnThreads / (D / 8)) {
+                const int row = row0 + 16 * nr + line;
+                if (row >= rows) break;
+                float z[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z[j] = 0.f;
+                float hi = kNoScore, l = 0.f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) hi = fmaxf(hi, wstat[w][16 * nr + line].x);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const float2 st = wstat[w][16 * nr + line];
+                    l += st.y * fast_exp2(st.x - hi);
+                    const float* m = &merge[w][line][8 * piece];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) z[j] += m[j];
+                }
+                if (whole) {
+                    const int j = row / s.rep;
+                    const int64_t t = sq.row + j, i = head * s.rep + row - j * s.rep;
+                    const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] *= inv;
+                    store8<T>(out + t * s.o_tok + i * s.o_head + 8 * piece, z);
+                    if (lse && piece == 0)
+                        lse[i * s.t + t] = l > 0.f ? (hi + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+                } else {
+                    store8<float>(part + ((int64_t)slot * ROWS + 16 * nr + line) * D + 8 * piece, z);
+                    if (piece == 0) stat[(int64_t)slot * ROWS + 16 * nr + line] = float2{hi, l};
+                }
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// Rows cut between workgroups: their partial rows added up in the order of
+// the keys.  One wave to a row: item (sequence, head, tile) blockIdx.x, row
+// 4 blockIdx.y + wave.
+template <typename T, int D, int NR, int UNIT>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheShape s, const int* lens,
+                                                         const int* starts, int max_tiles,
+                                                         int groups, const int* plan,
+                                                         const float2* stat, const float* part,
+                                                         T* out, float* lse) {
+    constexpr int ROWS = 16 * NR, E = D / 64;
+    const int lane = threadIdx.x & 63, line = blockIdx.y * 4 + (threadIdx.x >> 6);
+    const int per_seq = s.hkv * max_tiles;
+    const int b = blockIdx.x / per_seq, item = blockIdx.x - b * per_seq;
+    const int head = item / max_tiles, tile = item - head * max_tiles;
+    const Seq sq = seq_at(s, lens, starts, b);
+    const Runs<ROWS, UNIT> run(s, sq);
+    const int row = tile * ROWS + line;
+    if (tile >= run.tiles || row >= sq.fresh * s.rep) return;
+    const int each = (plan[s.b] + groups - 1) / groups;
+    const int f0 = plan[b] + (head * run.tiles + tile) * run.units, f1 = f0 + run.units;
+    const int w0 = f0 / each, w1 = (f1 - 1) / each;
+    if (w0 == w1) return;
+    const int first = 2 * w0 + (f0 > w0 * each ? 1 : 0);
+    auto slot = [&](int w) { return (int64_t)(w == w0 ? first : 2 * w) * ROWS + line; };
+    float hi = kNoScore;
+    for (int w = w0 + lane; w <= w1; w += 64) hi = fmaxf(hi, stat[slot(w)].x);
+    hi = wave_max(hi);
+    float l = 0.f, z[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) z[e] = 0.f;
+#pragma unroll 4
+    for (int w = w0; w <= w1; ++w) {
+        const int64_t at = slot(w);
+        const float2 st = stat[at];
+        const float k = fast_exp2(st.x - hi);
+        l += st.y * k;
+#pragma unroll
+        for (int e = 0; e < E; ++e) z[e] += part[at * D + E * lane + e] * k;
+    }
+    const int j = row / s.rep;
+    const int64_t t = sq.row + j, i = head * s.rep + row - j * s.rep;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    T* o = out + t * s.o_tok + i * s.o_head + E * lane;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = from_f32_rne<T>(z[e] * inv);
+    if (lse && lane == 0) lse[i * s.t + t] = l > 0.f ? (hi + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+}
+
+// Workgroups of the first launch: two on a CU.
+constexpr int kCacheGroups = 512;
+
+static int max_row_tiles(const CacheShape& s, int tiles) {
+    return (int)(((int64_t)s.rep * s.max_new + 16 * tiles - 1) / (16 * tiles));
+}
+
+bool cache_ws(const CacheShape& s, CacheWs* w) {
+    const int64_t rows = (int64_t)s.rep * s.max_new;
+    w->tiles = rows <= 16 ? 1 : rows <= 32 || s.dtype == PROXYATTN_F32 ? 2 : 4;
+    const int unit = 64 * (s.fp4 ? 4 : 2);
+    const int64_t units = (s.max_len + unit - 1) / unit;
+    const int64_t runs = (int64_t)s.b * s.hkv * max_row_tiles(s, w->tiles);
+    // a workgroup of 256 threads to each run in the second launch
+    if (rows > INT32_MAX || runs > INT32_MAX / 256 || runs * units > INT32_MAX) return false;
+    w->groups = (int)std::max<int64_t>(1, std::min<int64_t>(kCacheGroups, runs * units));
+    w->joined = units > 1;
+    auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    const size_t parts = (size_t)2 * w->groups * 16 * w->tiles;
+    size_t off = 0;
+    w->plan = off, off = up(off + (size_t)(s.b + 1) * 4);
+    w->stat = off, off = up(off + parts * 8);
+    w->part = off, off = up(off + parts * s.d * 4);
+    w->total = off;
+    return true;
+}
+
+template <typename T, int D, bool FP4, int NR>
+static void attention_as(const CacheShape& s, const void* q, const int* table, const int* lens,
+                         const int* starts, const PagePtrs& pg, void* out, float* lse, char* ws,
+                         const CacheWs& w, hipStream_t st) {
+    int* plan = (int*)(ws + w.plan);
+    float2* stat = (float2*)(ws + w.stat);
+    float* part = (float*)(ws + w.part);
+    cache_attn_kernel<T, FP4, D, NR><<<w.groups, kAttnThreads, 0, st>>>(
+        s, (const T*)q, table, lens, starts, pg, (T*)out, lse, plan, stat, part);
+    if (!w.joined) return;
+    constexpr int UNIT = 64 * key_tiles<FP4>();
+    const int mt = max_row_tiles(s, NR);
+    const int rows = std::min(16 * NR, s.rep * s.max_new);
+    const dim3 grid((unsigned)s.b * s.hkv * mt, (rows + 3) / 4);
+    cache_join_kernel<T, D, NR, UNIT><<<grid, 256, 0, st>>>(s, lens, starts, mt, w.groups, plan,
+                                                            stat, part, (T*)out, lse);
+}
+
+hipError_t launch_cache_attention(const CacheShape& s, const void* q, const int* table,
+                                  const int* lens, const int* starts, const PagePtrs& pg,
+                                  void* out, float* lse, char* ws, const CacheWs& w,
+                                  hipStream_t st) {
+    by_cache_type(s, [&](auto t, auto d, auto fp4) {
+        typedef typename decltype(t)::type T;
+        constexpr int D = decltype(d)::value;
+        constexpr bool F = decltype(fp4)::value;
+        if (w.tiles == 1)
+            attention_as<T, D, F, 1>(s, q, table, lens, starts, pg, out, lse, ws, w, st);
+        else if (w.tiles == 2)
+            attention_as<T, D, F, 2>(s, q, table, lens, starts, pg, out, lse, ws, w, st);
+        else if constexpr (sizeof(T) == 2)
+            attention_as<T, D, F, 4>(s, q, table, lens, starts, pg, out, lse, ws, w, st);
+    });
+    return hipGetLastError();
+}
+
+}  // namespace pa

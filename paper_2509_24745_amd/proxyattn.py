@@ -11,7 +11,8 @@ from __future__ import annotations
 import ctypes
 import math
 import os
-from dataclasses import dataclass
+from dataclasses import dataclass, replace
+from functools import cached_property
 
 import torch  # loaded first: the library then binds to torch's HIP runtime
 
@@ -26,6 +27,7 @@ F32 = 1
 E_OK, E_INVALID, E_UNSUPPORTED, E_WORKSPACE, E_HIP = 0, 1, 2, 3, 4
 TOPK_CONSTANT, TOPK_ROW_RATIO, LIST_ASCENDING = 0, 1, 2
 LIST_BAD_COUNT, LIST_BAD_INDEX, LIST_DUPLICATE = 1, 2, 4
+CACHE_SAME, CACHE_FP4 = 0, 1
 
 
 class proxyattn_problem(ctypes.Structure):
@@ -48,6 +50,49 @@ class proxyattn_problem(ctypes.Structure):
         ("o_head_stride", ctypes.c_int64),
         ("attn_order", ctypes.c_int32),
         ("attn_chunk_rows", ctypes.c_int32),
+    ]
+
+
+class proxyattn_rotary(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("rotary_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("table_len", ctypes.c_int32),
+        ("norm_eps", ctypes.c_double),
+        ("cos", ctypes.c_void_p),
+        ("sin", ctypes.c_void_p),
+        ("q_weight", ctypes.c_void_p),
+        ("k_weight", ctypes.c_void_p),
+        ("q_out_tok_stride", ctypes.c_int64),
+        ("q_out_head_stride", ctypes.c_int64),
+        ("k_out_tok_stride", ctypes.c_int64),
+        ("k_out_head_stride", ctypes.c_int64),
+    ]
+
+
+class proxyattn_cache(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("num_seqs", ctypes.c_int32),
+        ("num_tokens", ctypes.c_int32),
+        ("max_new", ctypes.c_int32),
+        ("max_len", ctypes.c_int32),
+        ("num_q_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("table_width", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("cache_type", ctypes.c_int32),
+        ("softmax_scale", ctypes.c_float),
+        ("q_tok_stride", ctypes.c_int64),
+        ("q_head_stride", ctypes.c_int64),
+        ("kv_tok_stride", ctypes.c_int64),
+        ("kv_head_stride", ctypes.c_int64),
+        ("o_tok_stride", ctypes.c_int64),
+        ("o_head_stride", ctypes.c_int64),
     ]
 
 
@@ -79,6 +124,12 @@ _SIGS = {
                                        + [ctypes.c_void_p] * 3 + [ctypes.c_size_t, ctypes.c_void_p],
     "proxyattn_block_sparse_prefill_blocked_noalloc": [ctypes.c_void_p] * 3 + [ctypes.c_size_t]
                                                       + [ctypes.c_void_p] * 5,
+    "proxyattn_norm_rotate": [ctypes.c_void_p] * 5 + [ctypes.c_int32] + [ctypes.c_void_p] * 3,
+    "proxyattn_cache_size": [ctypes.c_void_p] * 3,
+    "proxyattn_cache_append": [ctypes.c_void_p] * 14,
+    "proxyattn_cache_read": [ctypes.c_void_p] * 11,
+    "proxyattn_cache_workspace_size": [ctypes.c_void_p] * 2,
+    "proxyattn_cache_attention": [ctypes.c_void_p] * 12 + [ctypes.c_size_t, ctypes.c_void_p],
     "proxyattn_error_string": [ctypes.c_int],
     "proxyattn_last_error": [],
     "proxyattn_version": [],
@@ -448,6 +499,252 @@ def proxyattn_dense_prefill_blocked(prob: Problem, q, kv_blocked, out, lse, work
         _ptr(workspace), _nbytes(workspace) if workspace is not None else 0, _stream(stream)))
 
 
+# ---------------------------------------------------------------------------
+# around the prefill: norm and rotation, and the paged cache
+# ---------------------------------------------------------------------------
+# A decode step is a few launches of some microseconds, so these calls check
+# their tensors with as few queries as will do and keep their C structs.
+def _arg(x, n_elems: int, name: str, dtype, device: int, contiguous: bool = True) -> int | None:
+    """Checks a torch argument as _need does and returns its pointer (ints and
+    None as they are)."""
+    if x is None or isinstance(x, int):
+        return x
+    if n_elems > 0:
+        if x.dtype is not dtype:
+            raise ProxyAttnError(E_INVALID, f"{name}: dtype {x.dtype}, the call needs {dtype}")
+        packed = x.is_contiguous()
+        if not (packed and x.numel() >= n_elems):
+            _need(x, n_elems, name, dtype, contiguous)
+        if device < 0 or x.get_device() != device:
+            _need(x, n_elems, name, dtype, contiguous)
+    return x.data_ptr()
+
+
+@dataclass(frozen=True)
+class Rotary:
+    """Norm of each head and rotation by position (mirrors proxyattn_rotary).
+
+    cos, sin: fp32 [table_len, rotary_dim / 2] on the GPU (with rotary_dim);
+    q_weight, k_weight: [head_dim] in the problem's dtype, None for no norm."""
+
+    rotary_dim: int = 0
+    interleaved: bool = False
+    eps: float = 1e-6
+    cos: torch.Tensor | None = None
+    sin: torch.Tensor | None = None
+    q_weight: torch.Tensor | None = None
+    k_weight: torch.Tensor | None = None
+    q_out_tok_stride: int = 0
+    q_out_head_stride: int = 0
+    k_out_tok_stride: int = 0
+    k_out_head_stride: int = 0
+
+    @property
+    def table_len(self) -> int:
+        return self.cos.shape[0] if self.cos is not None else 0
+
+    @cached_property
+    def _c(self):
+        r = proxyattn_rotary()
+        r.struct_size = ctypes.sizeof(proxyattn_rotary)
+        r.rotary_dim, r.interleaved = self.rotary_dim, int(self.interleaved)
+        r.table_len, r.norm_eps = self.table_len, self.eps
+        r.cos, r.sin = _ptr(self.cos), _ptr(self.sin)
+        r.q_weight, r.k_weight = _ptr(self.q_weight), _ptr(self.k_weight)
+        r.q_out_tok_stride, r.q_out_head_stride = self.q_out_tok_stride, self.q_out_head_stride
+        r.k_out_tok_stride, r.k_out_head_stride = self.k_out_tok_stride, self.k_out_head_stride
+        return r
+
+
+def _arg_rotary(r: Rotary | None, d: int, dtype, device: int):
+    if r is None:
+        return None
+    if r.rotary_dim > 0:
+        if r.cos is not None and r.sin is not None and r.cos.shape[0] != r.sin.shape[0]:
+            raise ProxyAttnError(E_INVALID, f"sin: {r.sin.shape[0]} rows, cos has {r.table_len}")
+        n = r.table_len * (r.rotary_dim // 2)
+        _arg(r.cos, n, "cos", torch.float32, device)
+        _arg(r.sin, n, "sin", torch.float32, device)
+    _arg(r.q_weight, d, "q_weight", dtype, device)
+    _arg(r.k_weight, d, "k_weight", dtype, device)
+    return ctypes.byref(r._c)
+
+
+def proxyattn_norm_rotate(prob: Problem, rotary: Rotary, q, k, positions, first_position: int,
+                          q_out, k_out, stream=None):
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    n, hq, hkv, d = prob.seq_len, prob.num_q_heads, prob.num_kv_heads, prob.head_dim
+    dt = prob.torch_dtype
+    r = _arg_rotary(rotary, d, dt, dev)
+    args = [_arg(q, _span(n, hq, d, prob.q_tok_stride, prob.q_head_stride), "q", dt, dev, False),
+            _arg(k, _span(n, hkv, d, prob.kv_tok_stride, prob.kv_head_stride), "k", dt, dev, False),
+            _arg(positions, n, "positions", torch.int32, dev), int(first_position),
+            _arg(q_out, _span(n, hq, d, rotary.q_out_tok_stride, rotary.q_out_head_stride),
+                 "q_out", dt, dev, False),
+            _arg(k_out, _span(n, hkv, d, rotary.k_out_tok_stride, rotary.k_out_head_stride),
+                 "k_out", dt, dev, False)]
+    p = prob.c_struct()
+    _check(lib().proxyattn_norm_rotate(ctypes.byref(p), r, *args, _stream(stream)))
+
+
+@dataclass(frozen=True)
+class Cache:
+    """A paged cache and a call's batch (mirrors proxyattn_cache)."""
+
+    num_seqs: int
+    num_tokens: int
+    max_new: int
+    max_len: int
+    num_q_heads: int
+    num_kv_heads: int
+    head_dim: int
+    page_size: int
+    num_pages: int
+    table_width: int
+    dtype: str = "bf16"
+    cache_type: str = "same"   # "same" (the dtype) or "fp4"
+    softmax_scale: float = 0.0
+    q_tok_stride: int = 0
+    q_head_stride: int = 0
+    kv_tok_stride: int = 0
+    kv_head_stride: int = 0
+    o_tok_stride: int = 0
+    o_head_stride: int = 0
+
+    @cached_property
+    def torch_dtype(self):
+        return torch.bfloat16 if self.dtype == "bf16" else torch.float32
+
+    @cached_property
+    def page_dtype(self):
+        return torch.uint8 if self.cache_type == "fp4" else self.torch_dtype
+
+    @cached_property
+    def _c(self):
+        c = proxyattn_cache()
+        c.struct_size = ctypes.sizeof(proxyattn_cache)
+        for name in ("num_seqs", "num_tokens", "max_new", "max_len", "num_q_heads",
+                     "num_kv_heads", "head_dim", "page_size", "num_pages", "table_width",
+                     "softmax_scale", "q_tok_stride", "q_head_stride", "kv_tok_stride",
+                     "kv_head_stride", "o_tok_stride", "o_head_stride"):
+            setattr(c, name, getattr(self, name))
+        c.dtype = {"bf16": BF16, "fp32": F32}.get(self.dtype, 99)
+        c.cache_type = {"same": CACHE_SAME, "fp4": CACHE_FP4}.get(self.cache_type, 99)
+        return c
+
+    @cached_property
+    def _sizes(self):
+        """Elements that a call touches: q, kv, out spans; a page pool; its scales."""
+        t, hq, hkv, d = self.num_tokens, self.num_q_heads, self.num_kv_heads, self.head_dim
+        rows = self.num_pages * hkv * self.page_size
+        fp4 = self.cache_type == "fp4"
+        return (_span(t, hq, d, self.q_tok_stride, self.q_head_stride),
+                _span(t, hkv, d, self.kv_tok_stride, self.kv_head_stride),
+                _span(t, hq, d, self.o_tok_stride, self.o_head_stride),
+                rows * (d // 2 if fp4 else d), rows * (d // 32) if fp4 else 0)
+
+    @cached_property
+    def _packed_q(self) -> "Cache":
+        """The same with packed queries and outputs (a decode step's own)."""
+        strides = dict(q_tok_stride=0, q_head_stride=0, o_tok_stride=0, o_head_stride=0)
+        return replace(self, **strides)
+
+    @cached_property
+    def _workspace_bytes(self) -> int:
+        return proxyattn_cache_workspace_size(self)
+
+
+def proxyattn_cache_size(cache: Cache) -> tuple[int, int]:
+    """Bytes of k_pages (and of v_pages) and of k_scales (and of v_scales)."""
+    a, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(lib().proxyattn_cache_size(ctypes.byref(cache._c), ctypes.byref(a), ctypes.byref(b)))
+    return a.value, b.value
+
+
+def proxyattn_cache_workspace_size(cache: Cache) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().proxyattn_cache_workspace_size(ctypes.byref(cache._c), ctypes.byref(n)))
+    return n.value
+
+
+@dataclass(frozen=True)
+class Pages:
+    """The pools of a cache: k, v [num_pages, Hkv, page_size, d] (fp4: uint8
+    [..., d / 2]) and, with fp4, k_scales, v_scales uint8 [num_pages, Hkv, d / 32,
+    page_size]."""
+
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scales: torch.Tensor | None = None
+    v_scales: torch.Tensor | None = None
+
+    @classmethod
+    def empty(cls, cache: Cache, device="cuda") -> "Pages":
+        lead = (cache.num_pages, cache.num_kv_heads)
+        fp4 = cache.cache_type == "fp4"
+        row = cache.head_dim // 2 if fp4 else cache.head_dim
+        pools = [torch.empty((*lead, cache.page_size, row), dtype=cache.page_dtype, device=device)
+                 for _ in range(2)]
+        if fp4:
+            pools += [torch.empty((*lead, cache.head_dim // 32, cache.page_size),
+                                  dtype=torch.uint8, device=device) for _ in range(2)]
+        return cls(*pools)
+
+
+def _arg_batch(cache: Cache, page_table, seq_lens, new_start, pages: Pages, device: int):
+    """Pointers of page_table, seq_lens, new_start and the four pools."""
+    b, i32 = cache.num_seqs, torch.int32
+    _, _, _, pool, scales = cache._sizes
+    return (_arg(page_table, b * cache.table_width, "page_table", i32, device),
+            _arg(seq_lens, b, "seq_lens", i32, device),
+            _arg(new_start, b + 1, "new_start", i32, device),
+            _arg(pages.k, pool, "k_pages", cache.page_dtype, device),
+            _arg(pages.v, pool, "v_pages", cache.page_dtype, device),
+            _arg(pages.k_scales, scales, "k_scales", torch.uint8, device),
+            _arg(pages.v_scales, scales, "v_scales", torch.uint8, device))
+
+
+def proxyattn_cache_append(cache: Cache, rotary: Rotary | None, q, k, v, q_out, page_table,
+                           seq_lens, new_start, pages: Pages, stream=None):
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    dt = cache.torch_dtype
+    nq, nkv = cache._sizes[:2]
+    r = _arg_rotary(rotary, cache.head_dim, dt, dev)
+    out = _span(cache.num_tokens, cache.num_q_heads, cache.head_dim, rotary.q_out_tok_stride,
+                rotary.q_out_head_stride) if rotary is not None else 0
+    args = (_arg(q, nq, "q", dt, dev, False), _arg(k, nkv, "k", dt, dev, False),
+            _arg(v, nkv, "v", dt, dev, False), _arg(q_out, out, "q_out", dt, dev, False))
+    batch = _arg_batch(cache, page_table, seq_lens, new_start, pages, dev)
+    _check(lib().proxyattn_cache_append(ctypes.byref(cache._c), r, *args, *batch,
+                                        _stream(stream)))
+
+
+def proxyattn_cache_read(cache: Cache, page_table, seq_lens, new_start, pages: Pages, k_out,
+                         v_out, stream=None):
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    nkv = cache._sizes[1]
+    outs = (_arg(k_out, nkv, "k_out", cache.torch_dtype, dev, False),
+            _arg(v_out, nkv, "v_out", cache.torch_dtype, dev, False))
+    batch = _arg_batch(cache, page_table, seq_lens, new_start, pages, dev)
+    _check(lib().proxyattn_cache_read(ctypes.byref(cache._c), *batch, *outs, _stream(stream)))
+
+
+def proxyattn_cache_attention(cache: Cache, q, page_table, seq_lens, new_start, pages: Pages, out,
+                              lse, workspace, stream=None):
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    dt = cache.torch_dtype
+    nq, _, no, _, _ = cache._sizes
+    qp = _arg(q, nq, "q", dt, dev, False)
+    batch = _arg_batch(cache, page_table, seq_lens, new_start, pages, dev)
+    op = _arg(out, no, "out", dt, dev, False)
+    lp = _arg(lse, cache.num_q_heads * cache.num_tokens, "lse", torch.float32, dev)
+    _need_ws(workspace, cache._workspace_bytes)
+    _check(lib().proxyattn_cache_attention(
+        ctypes.byref(cache._c), qp, *batch, op, lp, _ptr(workspace),
+        _nbytes(workspace) if isinstance(workspace, torch.Tensor) else
+        (0 if workspace is None else cache._workspace_bytes), _stream(stream)))
+
+
 def proxyattn_version() -> str:
     return lib().proxyattn_version().decode()
 
@@ -480,4 +777,32 @@ def prefill(prob: Problem, q, k, v, gamma: float, min_budget_tokens: int = 0,
                             bufs.head_count, bufs.block_count, bufs.block_index, stream)
     proxyattn_block_sparse_prefill(prob, q, k, v, bufs.block_count, bufs.block_index, bufs.out,
                                    bufs.lse, bufs.workspace, stream)
+    return bufs
+
+
+class CacheBuffers:
+    """What a decode step of one cache writes besides its pages."""
+
+    def __init__(self, cache: Cache, device="cuda"):
+        t, hq, d = cache.num_tokens, cache.num_q_heads, cache.head_dim
+        self.cache = cache
+        self.workspace = torch.empty(max(cache._workspace_bytes, 16), dtype=torch.uint8,
+                                     device=device)
+        self.q = torch.empty((t, hq, d), dtype=cache.torch_dtype, device=device)
+        self.out = torch.empty((t, hq, d), dtype=cache.torch_dtype, device=device)
+        self.lse = torch.empty((hq, t), dtype=torch.float32, device=device)
+
+
+def decode(cache: Cache, rotary: Rotary, q, k, v, page_table, seq_lens, new_start, pages: Pages,
+           bufs: CacheBuffers | None = None, stream=None) -> CacheBuffers:
+    """One layer's step after the prefill: the batch's new tokens normed,
+    rotated and appended, then their attention over the cache (cache_append,
+    cache_attention).  The rotary's q_out strides and the cache's o strides are
+    the packed ones."""
+    bufs = bufs or CacheBuffers(cache, q.device)
+    proxyattn_cache_append(cache, rotary, q, k, v, bufs.q, page_table, seq_lens, new_start, pages,
+                           stream)
+    packed = cache._packed_q
+    proxyattn_cache_attention(packed, bufs.q, page_table, seq_lens, new_start, pages, bufs.out,
+                              bufs.lse, bufs.workspace, stream)
     return bufs
