@@ -34,6 +34,7 @@
 namespace pa {
 
 constexpr int kAttnThreads = 256;   // 4 waves
+constexpr int kCacheGroups = 512;   // workgroups at most: two on a CU
 // Below any score that a finite row gives: the reference before the first key.
 constexpr float kNoScore = -1e30f;
 // Scores above the reference by this much (log2) move it: the sums grow by
@@ -44,6 +45,11 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // 16-key tiles of a step: 64 keys in 4 bits, 32 otherwise.
 template <bool FP4> constexpr int key_tiles() { return FP4 ? 4 : 2; }
+
+// Units that a run's start counts for when the work is dealt: a workgroup's
+// time goes by the runs it starts as well as by the keys it reads.  They lie
+// before the run's first keys.
+constexpr int kStartUnits = 1;
 
 // A sequence of the batch as the header reads its arrays.
 struct Seq {
@@ -67,6 +73,7 @@ template <int ROWS, int UNIT> struct Runs {
     int tiles, units;
     __device__ __forceinline__ Runs(const CacheShape& s, const Seq& q)
         : tiles((q.fresh * s.rep + ROWS - 1) / ROWS), units(max(1, (q.len + UNIT - 1) / UNIT)) {}
+    __device__ __forceinline__ int flat() const { return units + kStartUnits; }
 };
 
 __device__ __forceinline__ int wave_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -85,7 +92,7 @@ __device__ __forceinline__ void find_unit(const CacheShape& s, const int* lens, 
     const int b0 = tid * chunk, b1 = min(b0 + chunk, s.b);
     auto count = [&](int b) {
         const Runs<ROWS, UNIT> r(s, seq_at(s, lens, starts, b));
-        return s.hkv * r.tiles * r.units;
+        return s.hkv * r.tiles * r.flat();
     };
     int mine = 0;
     for (int b = b0; b < b1; ++b) mine += count(b);
@@ -452,7 +459,7 @@ template <> __device__ __forceinline__ void store8<float>(float* p, const float 
 }
 
 template <typename T, bool FP4, int D, int NR>
-__global__ __launch_bounds__(kAttnThreads) void cache_attn_kernel(
+__global__ __launch_bounds__(kAttnThreads, NR == 1 && sizeof(T) == 2 ? 2 : 1) void cache_attn_kernel(
     CacheShape s, const T* qp, const int* table, const int* lens, const int* starts, PagePtrs pg,
     T* out, float* lse, int* plan, float2* stat, float* part) {
     typedef KeyStep<T, FP4, D> Keys;
@@ -467,24 +474,29 @@ __global__ __launch_bounds__(kAttnThreads) void cache_attn_kernel(
     int total, per, b, base;
     find_unit<ROWS, UNIT>(s, lens, starts, group == 0 ? plan : nullptr, gridDim.x, group, &total,
                           &per, &b, &base);
-    int64_t f = (int64_t)per * group;
+    const int64_t begin = (int64_t)per * group;
+    int64_t f = begin;
     const int64_t fend = min(f + per, (int64_t)total);
-    bool first = true;
     while (f < fend) {
         Seq sq = seq_at(s, lens, starts, b);
         sq.len = wave_uniform(sq.len);
         sq.row = wave_uniform(sq.row);
         sq.fresh = wave_uniform(sq.fresh);
         const Runs<ROWS, UNIT> run(s, sq);
-        if (f >= (int64_t)base + (int64_t)s.hkv * run.tiles * run.units) {   // on to the next
-            base += s.hkv * run.tiles * run.units;
+        const int64_t past = (int64_t)base + (int64_t)s.hkv * run.tiles * run.flat();
+        if (f >= past) {   // on to the next sequence
+            base = (int)past;
             ++b;
             continue;
         }
-        const int at = (int)(f - base), item = at / run.units, u0 = at - item * run.units;
-        const int u1 = (int)min((int64_t)run.units, u0 + (fend - f));
+        const int at = (int)(f - base), item = at / run.flat(), u = at - item * run.flat();
+        const int ahead = (int)min((int64_t)run.flat(), u + (fend - f));
         const int head = item / run.tiles, row0 = (item - head * run.tiles) * ROWS;
-        f += u1 - u0;
+        const int u0 = max(u - kStartUnits, 0), u1 = ahead - kStartUnits;
+        // a run that goes on from the workgroup before, or starts here
+        const int slot = 2 * group + (f - u + kStartUnits > begin ? 1 : 0);
+        f += ahead - u;
+        if (u1 <= 0) continue;
 
         // rows: (new token, query head of the KV head); row n of tile nr sees keys up to limit
         const int rows = sq.fresh * s.rep, newest = sq.len - sq.fresh;
@@ -587,8 +599,6 @@ __global__ __launch_bounds__(kAttnThreads) void cache_attn_kernel(
 
         // the four waves' rows together
         const bool whole = u0 == 0 && u1 == run.units;
-        const int slot = 2 * group + (first ? 0 : 1);
-        first = false;
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr) {
             sum[nr] = groups_sum(sum[nr]);
@@ -648,55 +658,82 @@ __global__ __launch_bounds__(kAttnThreads) void cache_attn_kernel(
 }
 
 // Rows cut between workgroups: their partial rows added up in the order of
-// the keys.  One wave to a row: item (sequence, head, tile) blockIdx.x, row
-// 4 blockIdx.y + wave.
+// the keys.  A workgroup to a row: run (sequence, head, tile) blockIdx.x, row
+// blockIdx.y of it.  D/4 threads hold a partial row, 256 / (D/4) partial rows
+// are read side by side, the first four of each before anything is known of
+// their references.
 template <typename T, int D, int NR, int UNIT>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheShape s, const int* lens,
                                                          const int* starts, int max_tiles,
                                                          int groups, const int* plan,
                                                          const float2* stat, const float* part,
                                                          T* out, float* lse) {
-    constexpr int ROWS = 16 * NR, E = D / 64;
-    const int lane = threadIdx.x & 63, line = blockIdx.y * 4 + (threadIdx.x >> 6);
+    constexpr int ROWS = 16 * NR, L4 = D / 4, SIDE = 256 / L4, EARLY = 4;
+    __shared__ float2 piece[kCacheGroups];
+    __shared__ float top[4];
+    __shared__ __align__(16) float side[SIDE][D];
+    __shared__ float side_sum[SIDE];
+    const int tid = threadIdx.x, e = tid % L4, k = tid / L4, line = blockIdx.y;
     const int per_seq = s.hkv * max_tiles;
     const int b = blockIdx.x / per_seq, item = blockIdx.x - b * per_seq;
     const int head = item / max_tiles, tile = item - head * max_tiles;
     const Seq sq = seq_at(s, lens, starts, b);
+    const int each = (int)(((int64_t)plan[s.b] + groups - 1) / groups);
+    const int base = plan[b];
     const Runs<ROWS, UNIT> run(s, sq);
     const int row = tile * ROWS + line;
     if (tile >= run.tiles || row >= sq.fresh * s.rep) return;
-    const int each = (plan[s.b] + groups - 1) / groups;
-    const int f0 = plan[b] + (head * run.tiles + tile) * run.units, f1 = f0 + run.units;
-    const int w0 = f0 / each, w1 = (f1 - 1) / each;
+    const int f0 = base + (head * run.tiles + tile) * run.flat() + kStartUnits;
+    const int w0 = f0 / each, w1 = (f0 + run.units - 1) / each;
     if (w0 == w1) return;
-    const int first = 2 * w0 + (f0 > w0 * each ? 1 : 0);
-    auto slot = [&](int w) { return (int64_t)(w == w0 ? first : 2 * w) * ROWS + line; };
+    const int n = w1 - w0 + 1, first = 2 * w0 + (f0 > w0 * each ? 1 : 0);
+    auto slot = [&](int i) { return (int64_t)(i ? 2 * (w0 + i) : first) * ROWS + line; };
+    f32x4 early[EARLY];
+#pragma unroll
+    for (int i = 0; i < EARLY; ++i)
+        early[i] = *reinterpret_cast<const f32x4*>(part + slot(min(k + i * SIDE, n - 1)) * D + 4 * e);
     float hi = kNoScore;
-    for (int w = w0 + lane; w <= w1; w += 64) hi = fmaxf(hi, stat[slot(w)].x);
+    for (int i = tid; i < n; i += 256) {
+        piece[i] = stat[slot(i)];
+        hi = fmaxf(hi, piece[i].x);
+    }
     hi = wave_max(hi);
-    float l = 0.f, z[E];
+    if ((tid & 63) == 0) top[tid >> 6] = hi;
+    __syncthreads();
+    hi = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    float l = 0.f;
+    f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < E; ++e) z[e] = 0.f;
+    for (int i = 0; i < EARLY; ++i)
+        if (k + i * SIDE < n) {
+            const float2 st = piece[k + i * SIDE];
+            const float x = fast_exp2(st.x - hi);
+            l += st.y * x;
+            z += early[i] * x;
+        }
 #pragma unroll 4
-    for (int w = w0; w <= w1; ++w) {
-        const int64_t at = slot(w);
-        const float2 st = stat[at];
-        const float k = fast_exp2(st.x - hi);
-        l += st.y * k;
+    for (int i = k + EARLY * SIDE; i < n; i += SIDE) {
+        const float2 st = piece[i];
+        const float x = fast_exp2(st.x - hi);
+        l += st.y * x;
+        z += *reinterpret_cast<const f32x4*>(part + slot(i) * D + 4 * e) * x;
+    }
+    *reinterpret_cast<f32x4*>(&side[k][4 * e]) = z;
+    if (e == 0) side_sum[k] = l;
+    __syncthreads();
+    if (tid >= D) return;
+    float sum = 0.f, o = 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) z[e] += part[at * D + E * lane + e] * k;
+    for (int i = 0; i < SIDE; ++i) {
+        sum += side_sum[i];
+        o += side[i][tid];
     }
     const int j = row / s.rep;
     const int64_t t = sq.row + j, i = head * s.rep + row - j * s.rep;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    T* o = out + t * s.o_tok + i * s.o_head + E * lane;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = from_f32_rne<T>(z[e] * inv);
-    if (lse && lane == 0) lse[i * s.t + t] = l > 0.f ? (hi + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
+    out[t * s.o_tok + i * s.o_head + tid] = from_f32_rne<T>(sum > 0.f ? o / sum : 0.f);
+    if (lse && tid == 0)
+        lse[i * s.t + t] = sum > 0.f ? (hi + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
 }
-
-// Workgroups of the first launch: two on a CU.
-constexpr int kCacheGroups = 512;
 
 static int max_row_tiles(const CacheShape& s, int tiles) {
     return (int)(((int64_t)s.rep * s.max_new + 16 * tiles - 1) / (16 * tiles));
@@ -706,11 +743,11 @@ bool cache_ws(const CacheShape& s, CacheWs* w) {
     const int64_t rows = (int64_t)s.rep * s.max_new;
     w->tiles = rows <= 16 ? 1 : rows <= 32 || s.dtype == PROXYATTN_F32 ? 2 : 4;
     const int unit = 64 * (s.fp4 ? 4 : 2);
-    const int64_t units = (s.max_len + unit - 1) / unit;
+    const int64_t units = (s.max_len + unit - 1) / unit, flat = units + kStartUnits;
     const int64_t runs = (int64_t)s.b * s.hkv * max_row_tiles(s, w->tiles);
     // a workgroup of 256 threads to each run in the second launch
-    if (rows > INT32_MAX || runs > INT32_MAX / 256 || runs * units > INT32_MAX) return false;
-    w->groups = (int)std::max<int64_t>(1, std::min<int64_t>(kCacheGroups, runs * units));
+    if (rows > INT32_MAX || runs > INT32_MAX / 256 || runs * flat > INT32_MAX) return false;
+    w->groups = (int)std::max<int64_t>(1, std::min<int64_t>(w->tiles == 1 ? kCacheGroups : kCacheGroups / 2, runs * flat));
     w->joined = units > 1;
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     const size_t parts = (size_t)2 * w->groups * 16 * w->tiles;
@@ -735,7 +772,7 @@ static void attention_as(const CacheShape& s, const void* q, const int* table, c
     constexpr int UNIT = 64 * key_tiles<FP4>();
     const int mt = max_row_tiles(s, NR);
     const int rows = std::min(16 * NR, s.rep * s.max_new);
-    const dim3 grid((unsigned)s.b * s.hkv * mt, (rows + 3) / 4);
+    const dim3 grid((unsigned)s.b * s.hkv * mt, rows);
     cache_join_kernel<T, D, NR, UNIT><<<grid, 256, 0, st>>>(s, lens, starts, mt, w.groups, plan,
                                                             stat, part, (T*)out, lse);
 }
