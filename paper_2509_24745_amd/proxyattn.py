@@ -507,17 +507,22 @@ def proxyattn_dense_prefill_blocked(prob: Problem, q, kv_blocked, out, lse, work
 def _arg(x, n_elems: int, name: str, dtype, device: int, contiguous: bool = True) -> int | None:
     """Checks a torch argument as _need does and returns its pointer (ints and
     None as they are)."""
-    if x is None or isinstance(x, int):
+    if x is None or type(x) is int:
         return x
-    if n_elems > 0:
-        if x.dtype is not dtype:
-            raise ProxyAttnError(E_INVALID, f"{name}: dtype {x.dtype}, the call needs {dtype}")
-        packed = x.is_contiguous()
-        if not (packed and x.numel() >= n_elems):
-            _need(x, n_elems, name, dtype, contiguous)
-        if device < 0 or x.get_device() != device:
-            _need(x, n_elems, name, dtype, contiguous)
+    if not (x.dtype is dtype and x.is_contiguous() and x.numel() >= n_elems
+            and x.get_device() == device >= 0):
+        _need(x, n_elems, name, dtype, contiguous)   # says what is wrong, or that nothing is
     return x.data_ptr()
+
+
+def _device_and_stream(stream) -> tuple[int, int | None]:
+    """The current device (-1: none) and the stream's handle."""
+    if not torch.cuda.is_available():
+        return -1, stream if stream is None or isinstance(stream, int) else stream.cuda_stream
+    dev = torch.cuda.current_device()
+    if stream is None:   # torch.cuda.current_stream() makes a Stream first, which takes longer
+        return dev, torch._C._cuda_getCurrentRawStream(dev)
+    return dev, stream if isinstance(stream, int) else stream.cuda_stream
 
 
 @dataclass(frozen=True)
@@ -572,7 +577,7 @@ def _arg_rotary(r: Rotary | None, d: int, dtype, device: int):
 
 def proxyattn_norm_rotate(prob: Problem, rotary: Rotary, q, k, positions, first_position: int,
                           q_out, k_out, stream=None):
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    dev, st = _device_and_stream(stream)
     n, hq, hkv, d = prob.seq_len, prob.num_q_heads, prob.num_kv_heads, prob.head_dim
     dt = prob.torch_dtype
     r = _arg_rotary(rotary, d, dt, dev)
@@ -584,7 +589,7 @@ def proxyattn_norm_rotate(prob: Problem, rotary: Rotary, q, k, positions, first_
             _arg(k_out, _span(n, hkv, d, rotary.k_out_tok_stride, rotary.k_out_head_stride),
                  "k_out", dt, dev, False)]
     p = prob.c_struct()
-    _check(lib().proxyattn_norm_rotate(ctypes.byref(p), r, *args, _stream(stream)))
+    _check(lib().proxyattn_norm_rotate(ctypes.byref(p), r, *args, st))
 
 
 @dataclass(frozen=True)
@@ -706,7 +711,7 @@ def _arg_batch(cache: Cache, page_table, seq_lens, new_start, pages: Pages, devi
 
 def proxyattn_cache_append(cache: Cache, rotary: Rotary | None, q, k, v, q_out, page_table,
                            seq_lens, new_start, pages: Pages, stream=None):
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    dev, st = _device_and_stream(stream)
     dt = cache.torch_dtype
     nq, nkv = cache._sizes[:2]
     r = _arg_rotary(rotary, cache.head_dim, dt, dev)
@@ -716,22 +721,22 @@ def proxyattn_cache_append(cache: Cache, rotary: Rotary | None, q, k, v, q_out, 
             _arg(v, nkv, "v", dt, dev, False), _arg(q_out, out, "q_out", dt, dev, False))
     batch = _arg_batch(cache, page_table, seq_lens, new_start, pages, dev)
     _check(lib().proxyattn_cache_append(ctypes.byref(cache._c), r, *args, *batch,
-                                        _stream(stream)))
+                                        st))
 
 
 def proxyattn_cache_read(cache: Cache, page_table, seq_lens, new_start, pages: Pages, k_out,
                          v_out, stream=None):
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    dev, st = _device_and_stream(stream)
     nkv = cache._sizes[1]
     outs = (_arg(k_out, nkv, "k_out", cache.torch_dtype, dev, False),
             _arg(v_out, nkv, "v_out", cache.torch_dtype, dev, False))
     batch = _arg_batch(cache, page_table, seq_lens, new_start, pages, dev)
-    _check(lib().proxyattn_cache_read(ctypes.byref(cache._c), *batch, *outs, _stream(stream)))
+    _check(lib().proxyattn_cache_read(ctypes.byref(cache._c), *batch, *outs, st))
 
 
 def proxyattn_cache_attention(cache: Cache, q, page_table, seq_lens, new_start, pages: Pages, out,
                               lse, workspace, stream=None):
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    dev, st = _device_and_stream(stream)
     dt = cache.torch_dtype
     nq, _, no, _, _ = cache._sizes
     qp = _arg(q, nq, "q", dt, dev, False)
@@ -742,7 +747,7 @@ def proxyattn_cache_attention(cache: Cache, q, page_table, seq_lens, new_start, 
     _check(lib().proxyattn_cache_attention(
         ctypes.byref(cache._c), qp, *batch, op, lp, _ptr(workspace),
         _nbytes(workspace) if isinstance(workspace, torch.Tensor) else
-        (0 if workspace is None else cache._workspace_bytes), _stream(stream)))
+        (0 if workspace is None else cache._workspace_bytes), st))
 
 
 def proxyattn_version() -> str:
