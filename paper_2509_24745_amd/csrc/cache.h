@@ -71,7 +71,7 @@ struct CacheWs {
     size_t part;   // partial outputs [2 W][rows][d] fp32
     size_t total;
     int groups;    // workgroups W
-    int tiles;     // 16-row tiles of a workgroup's rows: 1, 2 or 4
+    int tiles;     // 16-row tiles of a workgroup's rows: 1 to 4
     int joined;    // whether a (sequence, head) can be split over workgroups
 };
 // False: more units of work than an int counts.

@@ -34,7 +34,8 @@
 namespace pa {
 
 constexpr int kAttnThreads = 256;   // 4 waves
-constexpr int kCacheGroups = 512;   // workgroups at most: two on a CU
+constexpr int kCus = 256;
+constexpr int kCacheGroups = 2 * kCus;   // workgroups at most
 // Below any score that a finite row gives: the reference before the first key.
 constexpr float kNoScore = -1e30f;
 // Scores above the reference by this much (log2) move it: the sums grow by
@@ -43,8 +44,14 @@ constexpr float kSlack = 8.f;
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// 16-key tiles of a step: 64 keys in 4 bits, 32 otherwise.
-template <bool FP4> constexpr int key_tiles() { return FP4 ? 4 : 2; }
+// 16-key tiles of a step: 64 keys in 4 bits, 32 in bf16 and in fp32 up to 64
+// values, 16 otherwise, so that two steps' keys and values fit beside the rows.
+constexpr int key_tiles(bool fp4, int esz, int d) { return fp4 ? 4 : esz * d > 256 ? 1 : 2; }
+
+// Workgroups that a CU holds: as many as the registers allow.
+constexpr int groups_per_cu(bool fp4, int esz, int d, int nr) {
+    return nr == 1 || (nr == 2 && (fp4 || d == 64)) || (nr == 3 && !fp4 && d == 64) ? 2 : 1;
+}
 
 // Units that a run's start counts for when the work is dealt: a workgroup's
 // time goes by the runs it starts as well as by the keys it reads.  They lie
@@ -79,43 +86,58 @@ template <int ROWS, int UNIT> struct Runs {
 __device__ __forceinline__ int wave_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // Which sequence a flat unit lies in, its first unit, and the number of all
-// units.  A block of 256 threads; plan (not NULL): every sequence's first unit
-// is left there, the total behind them.
+// units.  A block of 256 threads.  plan (not NULL): every sequence's first unit
+// is left there, the total behind them.  seqs: the sequences, up to 256 of them.
+struct Found {
+    int begin, end, b, base;   // the workgroup's units; the sequence that begin lies in
+};
+// Workgroup w's first unit of `total`, and the workgroup that unit f is with.
+__device__ __forceinline__ int first_unit(int total, int groups, int w) {
+    return (int)((int64_t)w * total / groups);
+}
+__device__ __forceinline__ int group_of(int total, int groups, int f) {
+    return (int)((((int64_t)f + 1) * groups - 1) / total);
+}
 template <int ROWS, int UNIT>
-__device__ __forceinline__ void find_unit(const CacheShape& s, const int* lens, const int* starts,
-                                          int* plan, int64_t groups, int group, int* total,
-                                          int* per, int* b_out, int* base_out) {
-    __shared__ int wave_sum_[4];
+__device__ __forceinline__ Found find_unit(const CacheShape& s, const int* lens, const int* starts,
+                                           int* plan, int groups, int group, Seq* seqs) {
+    __shared__ int wave_total[4];
     __shared__ int found[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int chunk = (s.b + kAttnThreads - 1) / kAttnThreads;
-    const int b0 = tid * chunk, b1 = min(b0 + chunk, s.b);
-    auto count = [&](int b) {
-        const Runs<ROWS, UNIT> r(s, seq_at(s, lens, starts, b));
+    const int b0 = min(tid * chunk, s.b), b1 = min(b0 + chunk, s.b);
+    auto count = [&](const Seq& q) {
+        const Runs<ROWS, UNIT> r(s, q);
         return s.hkv * r.tiles * r.flat();
     };
     int mine = 0;
-    for (int b = b0; b < b1; ++b) mine += count(b);
+    for (int b = b0; b < b1; ++b) {
+        const Seq q = seq_at(s, lens, starts, b);
+        if (chunk == 1) seqs[tid] = q;
+        mine += count(q);
+    }
     int incl = mine;
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) {
         const int x = __shfl_up(incl, o);
         if (lane >= o) incl += x;
     }
-    if (lane == 63) wave_sum_[wave] = incl;
+    if (lane == 63) wave_total[wave] = incl;
     __syncthreads();
     int before = incl - mine, all = 0;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        if (w < wave) before += wave_sum_[w];
-        all += wave_sum_[w];
+        if (w < wave) before += wave_total[w];
+        all += wave_total[w];
     }
-    const int each = (int)((all + groups - 1) / groups);
-    const int64_t want = (int64_t)each * group;
-    if ((want >= before && want < before + mine) || (plan && mine)) {
+    groups = min(groups, all);   // a unit at least to each that has any
+    const bool any = group < groups;
+    const int want = any ? first_unit(all, groups, group) : all;
+    const int end = any ? first_unit(all, groups, group + 1) : all;
+    if (plan || (want >= before && want < before + mine)) {
         int at = before;
         for (int b = b0; b < b1; ++b) {
-            const int n = count(b);
+            const int n = chunk == 1 ? mine : count(seq_at(s, lens, starts, b));
             if (plan) plan[b] = at;
             if (want >= at && want < at + n) {
                 found[0] = b;
@@ -123,15 +145,10 @@ __device__ __forceinline__ void find_unit(const CacheShape& s, const int* lens, 
             }
             at += n;
         }
-    } else if (plan) {
-        for (int b = b0; b < b1; ++b) plan[b] = before;
     }
     if (plan && tid == 0) plan[s.b] = all;
     __syncthreads();
-    *total = all;
-    *per = each;
-    *b_out = want < all ? wave_uniform(found[0]) : 0;
-    *base_out = want < all ? wave_uniform(found[1]) : 0;
+    return {want, end, any ? wave_uniform(found[0]) : 0, any ? wave_uniform(found[1]) : 0};
 }
 
 // ---------------------------------------------------------------------------
@@ -142,7 +159,7 @@ template <typename T, bool FP4, int D> struct KeyStep;
 // The problem's own type.  Chunk i of a key is its values 16 B of which lane
 // group g holds: for bf16 8 values 32 i + 8 g, for fp32 4 values 16 i + 4 g.
 template <typename T, int D> struct KeyStep<T, false, D> {
-    static constexpr int KT = 2, N = 16 / sizeof(T);
+    static constexpr int KT = key_tiles(false, sizeof(T), D), N = 16 / sizeof(T);
     static constexpr int KC = D / 4 / N;              // 16-byte pieces of a key for a lane
     static constexpr int VW = D / 16 * sizeof(T) / 4; // words of a value row for a lane
     u32x4 k[KT][KC];
@@ -190,7 +207,7 @@ template <typename T, int D> struct KeyStep<T, false, D> {
 // 4 bits.  A lane holds the D/4 values (D/4) g .. of each of its keys, D/16 of
 // each of its values, and their scales.
 template <typename T, int D> struct KeyStep<T, true, D> {
-    static constexpr int KT = 4;
+    static constexpr int KT = key_tiles(true, sizeof(T), D);
     static constexpr int KC = D / 32;   // words of a key for a lane
     uint32_t k[KT][KC];
     uint32_t ks;        // scales of the lane's KT keys, a byte each
@@ -272,6 +289,49 @@ __device__ __forceinline__ uint32_t fp4_pair_bf16(uint32_t w, float scale, int b
 }
 __device__ __forceinline__ bf16x8 as_frag(const u32x4& w) { return __builtin_bit_cast(bf16x8, w); }
 
+// The queries of NR tiles of 16 rows.  Piece i of a row for lane group g is the
+// values that the group's part of a key holds.  One tile's stay in registers; several
+// tiles' lie in LDS, lines padded by 16 bytes so that 16 rows meet all banks, and
+// are read in every step: the registers hold the outputs and the next keys.
+template <typename T, bool FP4, int D, int NR> struct Queries {
+    static constexpr int N = 16 / sizeof(T), QC = D / 4 / N;   // pieces of 16 bytes
+    static constexpr int LINE = D + N;
+    static constexpr int LDS = NR == 1 ? 4 : 16 * NR * LINE;   // elements
+    static constexpr bool kept = NR == 1;
+    static __device__ __forceinline__ int piece_at(int i, int g) {
+        return FP4 ? D / 4 * g + N * i : 4 * N * i + N * g;
+    }
+    u32x4 reg[kept ? QC : 1];
+    const T* lds;
+
+    // row(n): row n of the tiles, or NULL for none
+    template <typename F> __device__ __forceinline__ void load(T* buf, int lane, F row) {
+        lds = buf;
+        if constexpr (kept) {
+            const T* p = row(lane & 15);
+#pragma unroll
+            for (int i = 0; i < QC; ++i) {
+                reg[i] = zero_u32x4();
+                if (p) reg[i] = *reinterpret_cast<const u32x4*>(p + piece_at(i, lane >> 4));
+            }
+        } else {
+            for (int x = threadIdx.x; x < 16 * NR * (D / N); x += kAttnThreads) {
+                const int n = x / (D / N), c = x % (D / N);
+                const T* p = row(n);
+                u32x4 w = zero_u32x4();
+                if (p) w = *reinterpret_cast<const u32x4*>(p + N * c);
+                *reinterpret_cast<u32x4*>(buf + n * LINE + N * c) = w;
+            }
+            __syncthreads();
+        }
+    }
+    __device__ __forceinline__ u32x4 piece(int nr, int i, int lane) const {
+        if constexpr (kept) return reg[i];
+        return *reinterpret_cast<const u32x4*>(lds + (16 * nr + (lane & 15)) * LINE +
+                                               piece_at(i, lane >> 4));
+    }
+};
+
 // The rows' side of the products for NR tiles of 16 rows, and a step.
 template <typename T, bool FP4, int D, int NR> struct Rows;
 
@@ -284,46 +344,46 @@ template <typename T, bool FP4, int D, int NR> struct Rows;
 template <bool FP4, int D, int NR> struct Rows<bf16, FP4, D, NR> {
     typedef KeyStep<bf16, FP4, D> Keys;
     static constexpr int KT = Keys::KT, QC = D / 32, OC = D / 16;
-    bf16x8 q[NR][QC];
+    Queries<bf16, FP4, D, NR> q;
     f32x4 o[NR][OC];
 
-    __device__ __forceinline__ void load_query(int nr, const bf16* row, int g) {
+    __device__ __forceinline__ void scores(const Keys& ks, int lane, f32x4 (&x)[NR][KT]) const {
 #pragma unroll
-        for (int i = 0; i < QC; ++i) {
-            u32x4 w = zero_u32x4();
-            if (row) w = *reinterpret_cast<const u32x4*>(row + (FP4 ? D / 4 * g + 8 * i
-                                                                    : 32 * i + 8 * g));
-            q[nr][i] = as_frag(w);
-        }
-    }
-    __device__ __forceinline__ void scores(const Keys& ks, f32x4 (&x)[NR][KT]) const {
+        for (int t0 = 0; t0 < KT; t0 += 2) {
+            if constexpr (NR > 1) __builtin_amdgcn_sched_barrier(0);
+            bf16x8 kf[2][QC];
 #pragma unroll
-        for (int t = 0; t < KT; ++t) {
-            bf16x8 kf[QC];
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int i = 0; i < QC; ++i) {
-                if constexpr (FP4) {
-                    u32x4 w;
-                    const float sc = ks.kscale(t);
+                for (int i = 0; i < QC; ++i) {
+                    if constexpr (FP4) {
+                        u32x4 w;
+                        const float sc = ks.kscale(t0 + t);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) w[j] = fp4_pair_bf16(ks.k[t][i], sc, j);
-                    kf[i] = as_frag(w);
-                } else {
-                    kf[i] = as_frag(ks.k[t][i]);
+                        for (int j = 0; j < 4; ++j) w[j] = fp4_pair_bf16(ks.k[t0 + t][i], sc, j);
+                        kf[t][i] = as_frag(w);
+                    } else {
+                        kf[t][i] = as_frag(ks.k[t0 + t][i]);
+                    }
                 }
-            }
 #pragma unroll
             for (int nr = 0; nr < NR; ++nr) {
-                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < QC; ++i) acc = mma16(kf[i], q[nr][i], acc);
-                x[nr][t] = acc;
+                for (int t = 0; t < 2; ++t) x[nr][t0 + t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < QC; ++i) {
+                    const bf16x8 qf = as_frag(q.piece(nr, i, lane));
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+                        x[nr][t0 + t] = mma16(kf[t][i], qf, x[nr][t0 + t]);
+                }
             }
         }
     }
     __device__ __forceinline__ void outputs(const Keys& ks, const f32x4 (&p)[NR][KT]) {
 #pragma unroll
         for (int u = 0; u < KT / 2; ++u) {
+            if constexpr (NR > 1) __builtin_amdgcn_sched_barrier(0);
             bf16x8 hi[NR], lo[NR];
 #pragma unroll
             for (int nr = 0; nr < NR; ++nr) {
@@ -339,6 +399,7 @@ template <bool FP4, int D, int NR> struct Rows<bf16, FP4, D, NR> {
                 hi[nr] = as_frag(h);
                 lo[nr] = as_frag(l);
             }
+            if constexpr (NR > 2) __builtin_amdgcn_sched_barrier(0);
             // slots 2 w, 2 w + 1 of the fragment: keys KT r + 2 u + w / 2, r = 2 (w % 2) and the next
 #pragma unroll
             for (int c = 0; c < OC / 2; ++c) {   // values 2 c and 2 c + 1 of the lane's
@@ -374,42 +435,38 @@ template <bool FP4, int D, int NR> struct Rows<bf16, FP4, D, NR> {
 // four times.
 template <bool FP4, int D, int NR> struct Rows<float, FP4, D, NR> {
     typedef KeyStep<float, FP4, D> Keys;
-    static constexpr int KT = Keys::KT, QC = D / 4, OC = D / 16;
-    float q[NR][QC];
+    static constexpr int KT = Keys::KT, QC = D / 16, OC = D / 16;
+    Queries<float, FP4, D, NR> q;
     f32x4 o[NR][OC];
 
-    __device__ __forceinline__ void load_query(int nr, const float* row, int g) {
+    __device__ __forceinline__ void scores(const Keys& ks, int lane, f32x4 (&x)[NR][KT]) const {
 #pragma unroll
-        for (int i = 0; i < QC / 4; ++i) {
-            f32x4 w = {0.f, 0.f, 0.f, 0.f};
-            if (row) w = *reinterpret_cast<const f32x4*>(row + (FP4 ? D / 4 * g + 4 * i
-                                                                    : 16 * i + 4 * g));
+        for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) q[nr][4 * i + j] = w[j];
-        }
-    }
-    __device__ __forceinline__ void scores(const Keys& ks, f32x4 (&x)[NR][KT]) const {
+            for (int t = 0; t < KT; ++t) x[nr][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int t = 0; t < KT; ++t) {
-            f32x4 acc[NR];
+        for (int i = 0; i < QC; i += 2) {
+            if constexpr (NR > 1) __builtin_amdgcn_sched_barrier(0);
+            u32x4 qf[NR][2];
 #pragma unroll
-            for (int nr = 0; nr < NR; ++nr) acc[nr] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-            for (int i = 0; i < QC / 8; ++i) {
+                for (int j = 0; j < 2; ++j) qf[nr][j] = q.piece(nr, i + j, lane);
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
                 float kf[8];
                 if constexpr (FP4) {
-                    fp4_values(ks.k[t][i], ks.kscale(t), kf);
+                    fp4_values(ks.k[t][i / 2], ks.kscale(t), kf);
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) kf[j] = __uint_as_float(ks.k[t][2 * i + j / 4][j % 4]);
+                    for (int j = 0; j < 8; ++j) kf[j] = __uint_as_float(ks.k[t][i + j / 4][j % 4]);
                 }
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
 #pragma unroll
-                    for (int nr = 0; nr < NR; ++nr) acc[nr] = mma16(kf[j], q[nr][8 * i + j], acc[nr]);
+                    for (int nr = 0; nr < NR; ++nr)
+                        x[nr][t] = mma16(kf[j], __uint_as_float(qf[nr][j / 4][j % 4]), x[nr][t]);
             }
-#pragma unroll
-            for (int nr = 0; nr < NR; ++nr) x[nr][t] = acc[nr];
         }
     }
     __device__ __forceinline__ void outputs(const Keys& ks, const f32x4 (&p)[NR][KT]) {
@@ -417,6 +474,7 @@ template <bool FP4, int D, int NR> struct Rows<float, FP4, D, NR> {
         for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
+                if constexpr (NR > 1) __builtin_amdgcn_sched_barrier(0);
                 const int x = KT * r + t;
                 float vf[OC];
                 if constexpr (FP4) {
@@ -459,7 +517,8 @@ template <> __device__ __forceinline__ void store8<float>(float* p, const float 
 }
 
 template <typename T, bool FP4, int D, int NR>
-__global__ __launch_bounds__(kAttnThreads, NR == 1 && sizeof(T) == 2 ? 2 : 1) void cache_attn_kernel(
+__global__ __launch_bounds__(kAttnThreads, groups_per_cu(FP4, sizeof(T), D, NR)) void
+cache_attn_kernel(
     CacheShape s, const T* qp, const int* table, const int* lens, const int* starts, PagePtrs pg,
     T* out, float* lse, int* plan, float2* stat, float* part) {
     typedef KeyStep<T, FP4, D> Keys;
@@ -467,34 +526,34 @@ __global__ __launch_bounds__(kAttnThreads, NR == 1 && sizeof(T) == 2 ? 2 : 1) vo
     constexpr int LINE = D + 4;   // a row's outputs in LDS, padded by a bank group
     __shared__ __align__(16) float merge[4][16][LINE];
     __shared__ float2 wstat[4][ROWS];
+    __shared__ __align__(16) T queries[Queries<T, FP4, D, NR>::LDS];
     const int lane = threadIdx.x & 63, wave = wave_uniform(threadIdx.x >> 6);
     const int g = lane >> 4, n = lane & 15;
     const int group = blockIdx.x;
 
-    int total, per, b, base;
-    find_unit<ROWS, UNIT>(s, lens, starts, group == 0 ? plan : nullptr, gridDim.x, group, &total,
-                          &per, &b, &base);
-    const int64_t begin = (int64_t)per * group;
-    int64_t f = begin;
-    const int64_t fend = min(f + per, (int64_t)total);
-    while (f < fend) {
-        Seq sq = seq_at(s, lens, starts, b);
+    __shared__ Seq seqs[kAttnThreads];
+    const Found found = find_unit<ROWS, UNIT>(s, lens, starts, group == 0 ? plan : nullptr,
+                                              gridDim.x, group, seqs);
+    int b = found.b, base = found.base;
+    int f = found.begin;
+    while (f < found.end) {
+        Seq sq = s.b <= kAttnThreads ? seqs[b] : seq_at(s, lens, starts, b);
         sq.len = wave_uniform(sq.len);
         sq.row = wave_uniform(sq.row);
         sq.fresh = wave_uniform(sq.fresh);
         const Runs<ROWS, UNIT> run(s, sq);
-        const int64_t past = (int64_t)base + (int64_t)s.hkv * run.tiles * run.flat();
+        const int past = base + s.hkv * run.tiles * run.flat();
         if (f >= past) {   // on to the next sequence
-            base = (int)past;
+            base = past;
             ++b;
             continue;
         }
-        const int at = (int)(f - base), item = at / run.flat(), u = at - item * run.flat();
-        const int ahead = (int)min((int64_t)run.flat(), u + (fend - f));
+        const int at = f - base, item = at / run.flat(), u = at - item * run.flat();
+        const int ahead = min(run.flat(), u + (found.end - f));
         const int head = item / run.tiles, row0 = (item - head * run.tiles) * ROWS;
         const int u0 = max(u - kStartUnits, 0), u1 = ahead - kStartUnits;
         // a run that goes on from the workgroup before, or starts here
-        const int slot = 2 * group + (f - u + kStartUnits > begin ? 1 : 0);
+        const int slot = 2 * group + (f - u + kStartUnits > found.begin ? 1 : 0);
         f += ahead - u;
         if (u1 <= 0) continue;
 
@@ -503,18 +562,16 @@ __global__ __launch_bounds__(kAttnThreads, NR == 1 && sizeof(T) == 2 ? 2 : 1) vo
         Rows<T, FP4, D, NR> r;
         int limit[NR];
         float ref[NR], sum[NR];
+        r.q.load(queries, lane, [&](int i) -> const T* {
+            const int row = row0 + i, j = row / s.rep;
+            return row < rows ? qp + (int64_t)(sq.row + j) * s.q_tok +
+                                    (int64_t)(head * s.rep + row - j * s.rep) * s.q_head
+                              : nullptr;
+        });
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr) {
             const int row = row0 + 16 * nr + n;
-            const int j = row / s.rep;
-            const T* q = nullptr;
-            limit[nr] = sq.len - 1;
-            if (row < rows) {
-                limit[nr] = newest + j;
-                q = qp + (int64_t)(sq.row + j) * s.q_tok +
-                    (int64_t)(head * s.rep + row - j * s.rep) * s.q_head;
-            }
-            r.load_query(nr, q, g);
+            limit[nr] = row < rows ? newest + row / s.rep : sq.len - 1;
             ref[nr] = kNoScore;
             sum[nr] = 0.f;
 #pragma unroll
@@ -534,7 +591,7 @@ __global__ __launch_bounds__(kAttnThreads, NR == 1 && sizeof(T) == 2 ? 2 : 1) vo
 
         auto step = [&](Keys& ks, int s0) {
             f32x4 x[NR][KT];
-            r.scores(ks, x);
+            r.scores(ks, lane, x);
             if (s0 + SK > sq.len) ks.drop_values(sq.len - (s0 + 4 * KT * g));
             const bool ends = s0 + SK - 1 > all_see;
 #pragma unroll
@@ -678,15 +735,15 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheShape s, const int
     const int b = blockIdx.x / per_seq, item = blockIdx.x - b * per_seq;
     const int head = item / max_tiles, tile = item - head * max_tiles;
     const Seq sq = seq_at(s, lens, starts, b);
-    const int each = (int)(((int64_t)plan[s.b] + groups - 1) / groups);
-    const int base = plan[b];
+    const int total = plan[s.b], base = plan[b];
+    groups = min(groups, total);
     const Runs<ROWS, UNIT> run(s, sq);
     const int row = tile * ROWS + line;
     if (tile >= run.tiles || row >= sq.fresh * s.rep) return;
     const int f0 = base + (head * run.tiles + tile) * run.flat() + kStartUnits;
-    const int w0 = f0 / each, w1 = (f0 + run.units - 1) / each;
+    const int w0 = group_of(total, groups, f0), w1 = group_of(total, groups, f0 + run.units - 1);
     if (w0 == w1) return;
-    const int n = w1 - w0 + 1, first = 2 * w0 + (f0 > w0 * each ? 1 : 0);
+    const int n = w1 - w0 + 1, first = 2 * w0 + (f0 > first_unit(total, groups, w0) ? 1 : 0);
     auto slot = [&](int i) { return (int64_t)(i ? 2 * (w0 + i) : first) * ROWS + line; };
     f32x4 early[EARLY];
 #pragma unroll
@@ -741,13 +798,14 @@ static int max_row_tiles(const CacheShape& s, int tiles) {
 
 bool cache_ws(const CacheShape& s, CacheWs* w) {
     const int64_t rows = (int64_t)s.rep * s.max_new;
-    w->tiles = rows <= 16 ? 1 : rows <= 32 || s.dtype == PROXYATTN_F32 ? 2 : 4;
-    const int unit = 64 * (s.fp4 ? 4 : 2);
+    const int esz = s.dtype == PROXYATTN_BF16 ? 2 : 4;
+    w->tiles = (int)std::min<int64_t>((rows + 15) / 16, esz == 2 ? 4 : 2);
+    const int unit = 64 * key_tiles(s.fp4, esz, s.d);
     const int64_t units = (s.max_len + unit - 1) / unit, flat = units + kStartUnits;
     const int64_t runs = (int64_t)s.b * s.hkv * max_row_tiles(s, w->tiles);
     // a workgroup of 256 threads to each run in the second launch
     if (rows > INT32_MAX || runs > INT32_MAX / 256 || runs * flat > INT32_MAX) return false;
-    w->groups = (int)std::max<int64_t>(1, std::min<int64_t>(w->tiles == 1 ? kCacheGroups : kCacheGroups / 2, runs * flat));
+    w->groups = (int)std::max<int64_t>(1, std::min<int64_t>(kCus * groups_per_cu(s.fp4, esz, s.d, w->tiles), runs * flat));
     w->joined = units > 1;
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     const size_t parts = (size_t)2 * w->groups * 16 * w->tiles;
@@ -769,7 +827,7 @@ static void attention_as(const CacheShape& s, const void* q, const int* table, c
     cache_attn_kernel<T, FP4, D, NR><<<w.groups, kAttnThreads, 0, st>>>(
         s, (const T*)q, table, lens, starts, pg, (T*)out, lse, plan, stat, part);
     if (!w.joined) return;
-    constexpr int UNIT = 64 * key_tiles<FP4>();
+    constexpr int UNIT = 64 * key_tiles(FP4, sizeof(T), D);
     const int mt = max_row_tiles(s, NR);
     const int rows = std::min(16 * NR, s.rep * s.max_new);
     const dim3 grid((unsigned)s.b * s.hkv * mt, rows);
@@ -789,8 +847,12 @@ hipError_t launch_cache_attention(const CacheShape& s, const void* q, const int*
             attention_as<T, D, F, 1>(s, q, table, lens, starts, pg, out, lse, ws, w, st);
         else if (w.tiles == 2)
             attention_as<T, D, F, 2>(s, q, table, lens, starts, pg, out, lse, ws, w, st);
-        else if constexpr (sizeof(T) == 2)
-            attention_as<T, D, F, 4>(s, q, table, lens, starts, pg, out, lse, ws, w, st);
+        else if constexpr (sizeof(T) == 2) {
+            if (w.tiles == 3)
+                attention_as<T, D, F, 3>(s, q, table, lens, starts, pg, out, lse, ws, w, st);
+            else
+                attention_as<T, D, F, 4>(s, q, table, lens, starts, pg, out, lse, ws, w, st);
+        }
     });
     return hipGetLastError();
 }
