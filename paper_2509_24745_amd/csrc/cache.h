@@ -32,6 +32,7 @@ struct CacheShape {
     int page_shift;  // log2(page_size)
     int num_pages, width;
     int dtype, fp4;
+    int past;        // the attention reads the pages past the caches
     float scale2;    // softmax scale times log2(e)
     int64_t q_tok, q_head, kv_tok, kv_head, o_tok, o_head;  // element strides
 };

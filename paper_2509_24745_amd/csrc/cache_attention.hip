@@ -156,6 +156,12 @@ __device__ __forceinline__ Found find_unit(const CacheShape& s, const int* lens,
 // ---------------------------------------------------------------------------
 template <typename T, bool FP4, int D> struct KeyStep;
 
+// A load, past the caches or not (see CacheShape::past).
+template <bool PAST, typename V> __device__ __forceinline__ V fetch(const void* p) {
+    if constexpr (PAST) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+    return *reinterpret_cast<const V*>(p);
+}
+
 // The problem's own type.  Chunk i of a key is its values 16 B of which lane
 // group g holds: for bf16 8 values 32 i + 8 g, for fp32 4 values 16 i + 4 g.
 template <typename T, int D> struct KeyStep<T, false, D> {
@@ -165,6 +171,7 @@ template <typename T, int D> struct KeyStep<T, false, D> {
     u32x4 k[KT][KC];
     uint32_t v[4 * KT][VW];
 
+    template <bool PAST>
     __device__ __forceinline__ void load(const CacheShape& s, const PagePtrs& pg, int kpage,
                                          int vpage, int head, int kpos, int vpos, int lane) {
         const int g = lane >> 4, m = lane & 15, mask = (1 << s.page_shift) - 1;
@@ -174,7 +181,7 @@ template <typename T, int D> struct KeyStep<T, false, D> {
         for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int i = 0; i < KC; ++i)
-                k[t][i] = *reinterpret_cast<const u32x4*>(kp + t * D + 4 * N * i);
+                k[t][i] = fetch<PAST, u32x4>(kp + t * D + 4 * N * i);
         const T* vp = (const T*)pg.v +
                       ((((int64_t)vpage * s.hkv + head) << s.page_shift) + (vpos & mask)) * D +
                       D / 16 * m;
@@ -183,12 +190,12 @@ template <typename T, int D> struct KeyStep<T, false, D> {
             if constexpr (VW % 4 == 0) {
 #pragma unroll
                 for (int i = 0; i < VW; i += 4) {
-                    const u32x4 w = *reinterpret_cast<const u32x4*>(vp + x * D + i * 4 / sizeof(T));
+                    const u32x4 w = fetch<PAST, u32x4>(vp + x * D + i * 4 / sizeof(T));
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v[x][i + j] = w[j];
                 }
             } else {
-                const u32x2 w = *reinterpret_cast<const u32x2*>(vp + x * D);
+                const u32x2 w = fetch<PAST, u32x2>(vp + x * D);
                 v[x][0] = w[0];
                 v[x][1] = w[1];
             }
@@ -214,6 +221,7 @@ template <typename T, int D> struct KeyStep<T, true, D> {
     uint32_t v[4 * KT]; // D = 64: the low half
     u32x4 vs;           // scales of the lane's 16 values
 
+    template <bool PAST>
     __device__ __forceinline__ void load(const CacheShape& s, const PagePtrs& pg, int kpage,
                                          int vpage, int head, int kpos, int vpos, int lane) {
         const int g = lane >> 4, m = lane & 15, mask = (1 << s.page_shift) - 1;
@@ -223,16 +231,16 @@ template <typename T, int D> struct KeyStep<T, true, D> {
 #pragma unroll
         for (int t = 0; t < KT; ++t) {
             if constexpr (KC == 4) {
-                const u32x4 w = *reinterpret_cast<const u32x4*>(kp + t * (D / 2));
+                const u32x4 w = fetch<PAST, u32x4>(kp + t * (D / 2));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) k[t][j] = w[j];
             } else {
-                const u32x2 w = *reinterpret_cast<const u32x2*>(kp + t * (D / 2));
+                const u32x2 w = fetch<PAST, u32x2>(kp + t * (D / 2));
                 k[t][0] = w[0];
                 k[t][1] = w[1];
             }
         }
-        ks = *reinterpret_cast<const uint32_t*>(
+        ks = fetch<PAST, uint32_t>(
             (const uint8_t*)pg.ks +
             ((kh * (D / 32) + g * (D / 4) / 32) << s.page_shift) + (kpos & mask));
         const uint8_t* vp = (const uint8_t*)pg.v +
@@ -240,11 +248,11 @@ template <typename T, int D> struct KeyStep<T, true, D> {
 #pragma unroll
         for (int x = 0; x < 4 * KT; ++x) {
             if constexpr (D == 128)
-                v[x] = *reinterpret_cast<const uint32_t*>(vp + x * (D / 2));
+                v[x] = fetch<PAST, uint32_t>(vp + x * (D / 2));
             else
-                v[x] = *reinterpret_cast<const uint16_t*>(vp + x * (D / 2));
+                v[x] = fetch<PAST, uint16_t>(vp + x * (D / 2));
         }
-        vs = *reinterpret_cast<const u32x4*>(
+        vs = fetch<PAST, u32x4>(
             (const uint8_t*)pg.vs +
             ((vh * (D / 32) + m * (D / 16) / 32) << s.page_shift) + (vpos & mask));
     }
@@ -516,7 +524,7 @@ template <> __device__ __forceinline__ void store8<float>(float* p, const float 
     *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
 }
 
-template <typename T, bool FP4, int D, int NR>
+template <typename T, bool FP4, int D, int NR, bool PAST>
 __global__ __launch_bounds__(kAttnThreads, groups_per_cu(FP4, sizeof(T), D, NR)) void
 cache_attn_kernel(
     CacheShape s, const T* qp, const int* table, const int* lens, const int* starts, PagePtrs pg,
@@ -634,20 +642,20 @@ cache_attn_kernel(
         if (s0 < key1) {
             Keys ka, kb;
             int kp = page(kpos(s0)), vp = page(vpos(s0));
-            auto fetch = [&](Keys& ks, int at_key) {   // at_key's pages are in kp, vp
+            auto read = [&](Keys& ks, int at_key) {   // at_key's pages are in kp, vp
                 const int kc = clamp_page(kp), vc = clamp_page(vp);
                 const int ahead = at_key + 4 * SK;
                 kp = page(kpos(ahead));
                 vp = page(vpos(ahead));
-                ks.load(s, pg, kc, vc, head, kpos(at_key), vpos(at_key), lane);
+                ks.template load<PAST>(s, pg, kc, vc, head, kpos(at_key), vpos(at_key), lane);
             };
-            fetch(ka, s0);
+            read(ka, s0);
             while (true) {
                 const int s1 = s0 + 4 * SK, s2 = s1 + 4 * SK;
-                if (s1 < key1) fetch(kb, s1);
+                if (s1 < key1) read(kb, s1);
                 step(ka, s0);
                 if (s1 >= key1) break;
-                if (s2 < key1) fetch(ka, s2);
+                if (s2 < key1) read(ka, s2);
                 step(kb, s1);
                 if (s2 >= key1) break;
                 s0 = s2;
@@ -824,8 +832,12 @@ static void attention_as(const CacheShape& s, const void* q, const int* table, c
     int* plan = (int*)(ws + w.plan);
     float2* stat = (float2*)(ws + w.stat);
     float* part = (float*)(ws + w.part);
-    cache_attn_kernel<T, FP4, D, NR><<<w.groups, kAttnThreads, 0, st>>>(
-        s, (const T*)q, table, lens, starts, pg, (T*)out, lse, plan, stat, part);
+    if (s.past)
+        cache_attn_kernel<T, FP4, D, NR, true><<<w.groups, kAttnThreads, 0, st>>>(
+            s, (const T*)q, table, lens, starts, pg, (T*)out, lse, plan, stat, part);
+    else
+        cache_attn_kernel<T, FP4, D, NR, false><<<w.groups, kAttnThreads, 0, st>>>(
+            s, (const T*)q, table, lens, starts, pg, (T*)out, lse, plan, stat, part);
     if (!w.joined) return;
     constexpr int UNIT = 64 * key_tiles(FP4, sizeof(T), D);
     const int mt = max_row_tiles(s, NR);
