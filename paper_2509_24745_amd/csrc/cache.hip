@@ -8,6 +8,7 @@
 #include "cache.h"
 #include "cache_device.h"
 #include "common.h"
+#include "internal.h"
 #include "proxyattn.h"
 
 namespace pa {
@@ -19,25 +20,47 @@ template <int D> struct RowLanes {
     static constexpr int rows = 64 / per_row;   // rows of a wave
 };
 
-// Outputs past this many bytes are stored past the caches: they would not stay in
-// L2 (8 x 4 MB) for their reader anyway, and the stores run faster (128K
-// tokens, 32 + 8 heads of 128, bf16: rotated in 565 instead of 575 us, read back from
-// 4 bits in 165 instead of 194).  Smaller ones stay for their reader.
-constexpr int64_t kPastCaches = (int64_t)32 << 20;
-
-__device__ __forceinline__ void put16(void* p, const u32x4& x, int past) {
-    if (past)
+// How a pass goes about the caches, by the bytes it writes.  More than L2 holds
+// (8 x 4 MB) would not stay there for its reader anyway and is stored past the
+// caches; where it is more than the MALL holds too, the rows are also loaded past them.
+// Neither, stores, both (us): 4K tokens, 40 heads of 128 rotated 24.0, 21.5, 27 (the
+// input still lies in the MALL); 128K tokens 588, 575, 565; 80K tokens appended in 4
+// bits and read back 485, 463, 439.  128K tokens read back from 4 bits: 160, 151.
+enum { kCached = 0, kStorePast = 1, kAllPast = 2 };
+static int how_past(int64_t bytes) {
+    return bytes > (int64_t)kMallBytes ? kAllPast : bytes > ((int64_t)32 << 20) ? kStorePast
+                                                                               : kCached;
+}
+template <int HOW> __device__ __forceinline__ void put16(void* p, const u32x4& x) {
+    if constexpr (HOW >= kStorePast)
         __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(p));
     else
         *reinterpret_cast<u32x4*>(p) = x;
+}
+template <int HOW> __device__ __forceinline__ u32x4 get16(const void* p) {
+    if constexpr (HOW == kAllPast)
+        return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+    else
+        return *reinterpret_cast<const u32x4*>(p);
+}
+// Calls f with `how` as a type.
+template <typename F> static void by_how(int how, F f) {
+    if (how == kAllPast)
+        f(std::integral_constant<int, kAllPast>());
+    else if (how == kStorePast)
+        f(std::integral_constant<int, kStorePast>());
+    else
+        f(std::integral_constant<int, kCached>());
 }
 
 // Eight consecutive values.
 template <typename T> struct Chunk;
 template <> struct Chunk<bf16> {
     u32x4 w;
-    __device__ __forceinline__ void load(const bf16* p) { w = *reinterpret_cast<const u32x4*>(p); }
-    __device__ __forceinline__ void store(bf16* p, int past) const { put16(p, w, past); }
+    template <int HOW = kCached> __device__ __forceinline__ void load(const bf16* p) {
+        w = get16<HOW>(p);
+    }
+    template <int HOW> __device__ __forceinline__ void store(bf16* p) const { put16<HOW>(p, w); }
     __device__ __forceinline__ float at(int e) const { return get_elem<bf16>(w, e); }
     __device__ __forceinline__ void from(const float (&x)[8]) {
 #pragma unroll
@@ -46,13 +69,13 @@ template <> struct Chunk<bf16> {
 };
 template <> struct Chunk<float> {
     f32x4 a, b;
-    __device__ __forceinline__ void load(const float* p) {
-        a = *reinterpret_cast<const f32x4*>(p);
-        b = *reinterpret_cast<const f32x4*>(p + 4);
+    template <int HOW = kCached> __device__ __forceinline__ void load(const float* p) {
+        a = __builtin_bit_cast(f32x4, get16<HOW>(p));
+        b = __builtin_bit_cast(f32x4, get16<HOW>(p + 4));
     }
-    __device__ __forceinline__ void store(float* p, int past) const {
-        put16(p, __builtin_bit_cast(u32x4, a), past);
-        put16(p + 4, __builtin_bit_cast(u32x4, b), past);
+    template <int HOW> __device__ __forceinline__ void store(float* p) const {
+        put16<HOW>(p, __builtin_bit_cast(u32x4, a));
+        put16<HOW>(p + 4, __builtin_bit_cast(u32x4, b));
     }
     __device__ __forceinline__ float at(int e) const { return e < 4 ? a[e & 3] : b[e & 3]; }
     __device__ __forceinline__ void from(const float (&x)[8]) {
@@ -161,9 +184,9 @@ __device__ __forceinline__ void turn_row(const Chunk<T>& a, const Chunk<T>& b,
 // ---------------------------------------------------------------------------
 // A workgroup takes 2^shift tokens, all heads; consecutive rows of a wave are
 // consecutive tokens of one head.
-template <typename T, int D>
+template <typename T, int D, int HOW>
 __global__ __launch_bounds__(kRowThreads) void norm_rotate_kernel(RotateRows w, RotaryArgs r,
-                                                                  int shift, int past) {
+                                                                  int shift) {
     constexpr int RW = RowLanes<D>::rows, LR = RowLanes<D>::per_row;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int in_row = lane % LR;
@@ -182,8 +205,8 @@ __global__ __launch_bounds__(kRowThreads) void norm_rotate_kernel(RotateRows w, 
         T* y = is_k ? (T*)w.ko + tc * w.ko_tok + (hc - nq) * w.ko_head
                     : (T*)w.qo + tc * w.qo_tok + hc * w.qo_head;
         Chunk<T> a, b;
-        a.load(x + 8 * lc.c0);
-        b.load(x + 8 * lc.c1);
+        a.template load<HOW>(x + 8 * lc.c0);
+        b.template load<HOW>(x + 8 * lc.c1);
         int pos = 0;
         if (r.rot) {
             pos = w.positions ? w.positions[tc] : w.first + tc;
@@ -196,8 +219,8 @@ __global__ __launch_bounds__(kRowThreads) void norm_rotate_kernel(RotateRows w, 
         if (live) {
             a.from(z0);
             b.from(z1);
-            a.store(y + 8 * lc.c0, past);
-            b.store(y + 8 * lc.c1, past);
+            a.template store<HOW>(y + 8 * lc.c0);
+            b.template store<HOW>(y + 8 * lc.c1);
         }
     }
 }
@@ -205,7 +228,9 @@ __global__ __launch_bounds__(kRowThreads) void norm_rotate_kernel(RotateRows w, 
 // Tokens to a workgroup (as a power of two, at most four) and workgroups along
 // a token's rows, `fill` workgroups in all where there is work for them.
 // 128K tokens, 40 heads: rotated in 645, 602, 565, 570 and 586 us with 1, 2, 4,
-// 8 and 16 tokens; 4K tokens 24.2 us with 1044 workgroups, 21.5 with 4176.
+// 8 and 16 tokens; 4K tokens 24.2 us with 1044 workgroups, 21.5 with 4176 (but 80K
+// tokens appended 473 us with one workgroup to four tokens, 596 with four, which
+// each look the slots up).
 static void row_grid(int tokens, int row_steps, int fill, int* shift, dim3* grid) {
     const int sh = tokens >= 2048 ? 2 : tokens >= 1024 ? 1 : 0;
     const int gx = (tokens + (1 << sh) - 1) >> sh;
@@ -223,11 +248,13 @@ static void norm_rotate_d(const RotateRows& w, const RotaryArgs& r, hipStream_t 
     dim3 grid;
     const int rw = 4 * 1024 / w.d;   // rows of a workgroup's round
     row_grid(w.n, (rows + rw - 1) / rw, 4096, &shift, &grid);
-    const int past = (int64_t)w.n * rows * w.d * (int)sizeof(T) > kPastCaches;
-    if (w.d == 64)
-        norm_rotate_kernel<T, 64><<<grid, kRowThreads, 0, st>>>(w, r, shift, past);
-    else
-        norm_rotate_kernel<T, 128><<<grid, kRowThreads, 0, st>>>(w, r, shift, past);
+    by_how(how_past((int64_t)w.n * rows * w.d * (int)sizeof(T)), [&](auto how) {
+        constexpr int HOW = decltype(how)::value;
+        if (w.d == 64)
+            norm_rotate_kernel<T, 64, HOW><<<grid, kRowThreads, 0, st>>>(w, r, shift);
+        else
+            norm_rotate_kernel<T, 128, HOW><<<grid, kRowThreads, 0, st>>>(w, r, shift);
+    });
 }
 
 hipError_t launch_norm_rotate(const RotateRows& w, const RotaryArgs& r, hipStream_t st) {
@@ -330,10 +357,10 @@ __device__ __forceinline__ void store_fp4(uint8_t* codes, uint8_t* scales, const
 // Queries to q_out, keys and values into their pages.  Units of a workgroup:
 // RW rows of queries, of keys or of values; consecutive rows are consecutive
 // tokens of a head, whose codes and scales are neighbours in a page.
-template <typename T, int D, bool FP4>
+template <typename T, int D, bool FP4, int HOW>
 __global__ __launch_bounds__(kRowThreads) void cache_append_kernel(
     CacheShape s, RotaryArgs r, AppendArgs a, const int* table, const int* lens, const int* starts,
-    PagePtrs pg, int shift, int past) {
+    PagePtrs pg, int shift) {
     constexpr int RW = RowLanes<D>::rows, LR = RowLanes<D>::per_row;
     constexpr int LINE = D + 4;   // a row's values in LDS, padded by a bank group
     __shared__ Slot slots[4];
@@ -362,8 +389,8 @@ __global__ __launch_bounds__(kRowThreads) void cache_append_kernel(
         const int c0 = turn ? lc.c0 : FP4 ? 2 * in_row : in_row;
         const int c1 = turn ? lc.c1 : FP4 ? 2 * in_row + 1 : in_row + LR;
         Chunk<T> lo, hi;
-        lo.load(x + 8 * c0);
-        hi.load(x + 8 * c1);
+        lo.template load<HOW>(x + 8 * c0);
+        hi.template load<HOW>(x + 8 * c1);
         float z[16];
         if (turn) {
             const int64_t at_pos = (int64_t)max(at.pos, 0) * (r.rot / 2);
@@ -376,8 +403,8 @@ __global__ __launch_bounds__(kRowThreads) void cache_append_kernel(
         if (part == 0) {
             if (live) {
                 T* y = (T*)a.qo + t * a.qo_tok + h * a.qo_head;
-                lo.store(y + 8 * c0, past);
-                hi.store(y + 8 * c1, past);
+                lo.template store<HOW>(y + 8 * c0);
+                hi.template store<HOW>(y + 8 * c1);
             }
             continue;
         }
@@ -411,19 +438,18 @@ __global__ __launch_bounds__(kRowThreads) void cache_append_kernel(
         } else if (live) {
             T* y = (T*)(part == 1 ? pg.k : pg.v) +
                    ((((int64_t)at.page * s.hkv + h) << s.page_shift) + at.slot) * D;
-            lo.store(y + 8 * c0, past);
-            hi.store(y + 8 * c1, past);
+            lo.template store<HOW>(y + 8 * c0);
+            hi.template store<HOW>(y + 8 * c1);
         }
     }
 }
 
 // Rows of the pages back in the problem's dtype.
-template <typename T, int D, bool FP4>
+template <typename T, int D, bool FP4, int HOW>
 __global__ __launch_bounds__(kRowThreads) void cache_read_kernel(CacheShape s, const int* table,
                                                                  const int* lens,
                                                                  const int* starts, PagePtrs pg,
-                                                                 T* ko, T* vo, int shift,
-                                                                 int past) {
+                                                                 T* ko, T* vo, int shift) {
     constexpr int RW = RowLanes<D>::rows, LR = RowLanes<D>::per_row;
     __shared__ Slot slots[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -460,8 +486,8 @@ __global__ __launch_bounds__(kRowThreads) void cache_read_kernel(CacheShape s, c
             hi.load(x + 8 * LR);
         }
         T* y = out + (int64_t)(t0 + (row & mask)) * s.kv_tok + h * s.kv_head + 8 * in_row;
-        lo.store(y, past);
-        hi.store(y + 8 * LR, past);
+        lo.template store<HOW>(y);
+        hi.template store<HOW>(y + 8 * LR);
     }
 }
 
@@ -473,10 +499,11 @@ static void append_as(const CacheShape& s, const RotaryArgs& r, const AppendArgs
     dim3 grid;
     const int rw = 4 * 1024 / D;
     row_grid(s.t, ((a.q ? s.hq : 0) + 2 * s.hkv + rw - 1) / rw, 1024, &shift, &grid);
-    const int past = (int64_t)s.t * ((a.q ? s.hq : 0) + (FP4 ? 0 : 2 * s.hkv)) * D * (int)sizeof(T) >
-                     kPastCaches;
-    cache_append_kernel<T, D, FP4><<<grid, kRowThreads, 0, st>>>(s, r, a, table, lens, starts, pg,
-                                                                 shift, past);
+    const int64_t rows = (int64_t)s.t * ((a.q ? s.hq : 0) + (FP4 ? 0 : 2 * s.hkv));
+    by_how(how_past(rows * D * (int)sizeof(T)), [&](auto how) {
+        cache_append_kernel<T, D, FP4, decltype(how)::value>
+            <<<grid, kRowThreads, 0, st>>>(s, r, a, table, lens, starts, pg, shift);
+    });
 }
 template <typename T, int D, bool FP4>
 static void read_as(const CacheShape& s, const int* table, const int* lens, const int* starts,
@@ -485,9 +512,10 @@ static void read_as(const CacheShape& s, const int* table, const int* lens, cons
     dim3 grid;
     const int rw = 4 * 1024 / D;
     row_grid(s.t, (2 * s.hkv + rw - 1) / rw, 1024, &shift, &grid);
-    const int past = (int64_t)s.t * 2 * s.hkv * D * (int)sizeof(T) > kPastCaches;
-    cache_read_kernel<T, D, FP4><<<grid, kRowThreads, 0, st>>>(s, table, lens, starts, pg, (T*)ko,
-                                                               (T*)vo, shift, past);
+    by_how(how_past((int64_t)s.t * 2 * s.hkv * D * (int)sizeof(T)), [&](auto how) {
+        cache_read_kernel<T, D, FP4, decltype(how)::value><<<grid, kRowThreads, 0, st>>>(
+            s, table, lens, starts, pg, (T*)ko, (T*)vo, shift);
+    });
 }
 
 hipError_t launch_cache_append(const CacheShape& s, const RotaryArgs& r, const AppendArgs& a,
