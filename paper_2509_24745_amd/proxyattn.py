@@ -515,17 +515,28 @@ def _arg(x, n_elems: int, name: str, dtype, device: int, contiguous: bool = True
     return x.data_ptr()
 
 
+_gpu_seen = False
+
+
 def _device_and_stream(stream) -> tuple[int, int | None]:
     """The current device (-1: none) and the stream's handle."""
-    if not torch.cuda.is_available():
-        return -1, stream if stream is None or isinstance(stream, int) else stream.cuda_stream
+    global _gpu_seen
+    if not _gpu_seen:
+        _gpu_seen = torch.cuda.is_available()
+        if not _gpu_seen:
+            return -1, stream if stream is None or isinstance(stream, int) else stream.cuda_stream
     dev = torch.cuda.current_device()
     if stream is None:   # torch.cuda.current_stream() makes a Stream first, which takes longer
         return dev, torch._C._cuda_getCurrentRawStream(dev)
     return dev, stream if isinstance(stream, int) else stream.cuda_stream
 
 
-@dataclass(frozen=True)
+def _same(tensors, checked) -> bool:
+    """Whether tensors that a descriptor holds still lie where they were checked."""
+    return checked is not None and checked == tuple(_ptr(x) for x in tensors)
+
+
+@dataclass(frozen=True, eq=False)
 class Rotary:
     """Norm of each head and rotation by position (mirrors proxyattn_rotary).
 
@@ -548,7 +559,7 @@ class Rotary:
     def table_len(self) -> int:
         return self.cos.shape[0] if self.cos is not None else 0
 
-    @cached_property
+    @property
     def _c(self):
         r = proxyattn_rotary()
         r.struct_size = ctypes.sizeof(proxyattn_rotary)
@@ -560,19 +571,26 @@ class Rotary:
         r.k_out_tok_stride, r.k_out_head_stride = self.k_out_tok_stride, self.k_out_head_stride
         return r
 
-
-def _arg_rotary(r: Rotary | None, d: int, dtype, device: int):
-    if r is None:
-        return None
-    if r.rotary_dim > 0:
-        if r.cos is not None and r.sin is not None and r.cos.shape[0] != r.sin.shape[0]:
-            raise ProxyAttnError(E_INVALID, f"sin: {r.sin.shape[0]} rows, cos has {r.table_len}")
-        n = r.table_len * (r.rotary_dim // 2)
-        _arg(r.cos, n, "cos", torch.float32, device)
-        _arg(r.sin, n, "sin", torch.float32, device)
-    _arg(r.q_weight, d, "q_weight", dtype, device)
-    _arg(r.k_weight, d, "k_weight", dtype, device)
-    return ctypes.byref(r._c)
+    def _arg(self, d: int, dtype, device: int):
+        """The struct, by reference; its tensors checked once for a use (and
+        again should they have moved)."""
+        key, tensors = (d, dtype, device), (self.cos, self.sin, self.q_weight, self.k_weight)
+        held = self.__dict__.get("_held")
+        if held is not None and held[0] == key and _same(tensors, held[1]):
+            return held[2]
+        if self.rotary_dim > 0:
+            if (self.cos is not None and self.sin is not None
+                    and self.cos.shape[0] != self.sin.shape[0]):
+                raise ProxyAttnError(E_INVALID, f"sin: {self.sin.shape[0]} rows, cos has "
+                                                f"{self.table_len}")
+            n = self.table_len * (self.rotary_dim // 2)
+            _arg(self.cos, n, "cos", torch.float32, device)
+            _arg(self.sin, n, "sin", torch.float32, device)
+        _arg(self.q_weight, d, "q_weight", dtype, device)
+        _arg(self.k_weight, d, "k_weight", dtype, device)
+        ref = ctypes.byref(self._c)
+        self.__dict__["_held"] = (key, tuple(_ptr(x) for x in tensors), ref)
+        return ref
 
 
 def proxyattn_norm_rotate(prob: Problem, rotary: Rotary, q, k, positions, first_position: int,
@@ -580,14 +598,15 @@ def proxyattn_norm_rotate(prob: Problem, rotary: Rotary, q, k, positions, first_
     dev, st = _device_and_stream(stream)
     n, hq, hkv, d = prob.seq_len, prob.num_q_heads, prob.num_kv_heads, prob.head_dim
     dt = prob.torch_dtype
-    r = _arg_rotary(rotary, d, dt, dev)
-    args = [_arg(q, _span(n, hq, d, prob.q_tok_stride, prob.q_head_stride), "q", dt, dev, False),
+    r = rotary._arg(d, dt, dev) if rotary is not None else None
+    nqo = nko = 0
+    if rotary is not None:
+        nqo = _span(n, hq, d, rotary.q_out_tok_stride, rotary.q_out_head_stride)
+        nko = _span(n, hkv, d, rotary.k_out_tok_stride, rotary.k_out_head_stride)
+    args = (_arg(q, _span(n, hq, d, prob.q_tok_stride, prob.q_head_stride), "q", dt, dev, False),
             _arg(k, _span(n, hkv, d, prob.kv_tok_stride, prob.kv_head_stride), "k", dt, dev, False),
             _arg(positions, n, "positions", torch.int32, dev), int(first_position),
-            _arg(q_out, _span(n, hq, d, rotary.q_out_tok_stride, rotary.q_out_head_stride),
-                 "q_out", dt, dev, False),
-            _arg(k_out, _span(n, hkv, d, rotary.k_out_tok_stride, rotary.k_out_head_stride),
-                 "k_out", dt, dev, False)]
+            _arg(q_out, nqo, "q_out", dt, dev, False), _arg(k_out, nko, "k_out", dt, dev, False))
     p = prob.c_struct()
     _check(lib().proxyattn_norm_rotate(ctypes.byref(p), r, *args, st))
 
@@ -623,6 +642,10 @@ class Cache:
     @cached_property
     def page_dtype(self):
         return torch.uint8 if self.cache_type == "fp4" else self.torch_dtype
+
+    @cached_property
+    def _ref(self):
+        return ctypes.byref(self._c)
 
     @cached_property
     def _c(self):
@@ -662,17 +685,17 @@ class Cache:
 def proxyattn_cache_size(cache: Cache) -> tuple[int, int]:
     """Bytes of k_pages (and of v_pages) and of k_scales (and of v_scales)."""
     a, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
-    _check(lib().proxyattn_cache_size(ctypes.byref(cache._c), ctypes.byref(a), ctypes.byref(b)))
+    _check(lib().proxyattn_cache_size(cache._ref, ctypes.byref(a), ctypes.byref(b)))
     return a.value, b.value
 
 
 def proxyattn_cache_workspace_size(cache: Cache) -> int:
     n = ctypes.c_size_t(0)
-    _check(lib().proxyattn_cache_workspace_size(ctypes.byref(cache._c), ctypes.byref(n)))
+    _check(lib().proxyattn_cache_workspace_size(cache._ref, ctypes.byref(n)))
     return n.value
 
 
-@dataclass(frozen=True)
+@dataclass(frozen=True, eq=False)
 class Pages:
     """The pools of a cache: k, v [num_pages, Hkv, page_size, d] (fp4: uint8
     [..., d / 2]) and, with fp4, k_scales, v_scales uint8 [num_pages, Hkv, d / 32,
@@ -695,18 +718,29 @@ class Pages:
                                   dtype=torch.uint8, device=device) for _ in range(2)]
         return cls(*pools)
 
+    def _args(self, cache: Cache, device: int):
+        """Pointers of the pools, checked once for a size (and again should
+        they have moved)."""
+        _, _, _, pool, scales = cache._sizes
+        key = (pool, scales, cache.page_dtype, device)
+        tensors = (self.k, self.v, self.k_scales, self.v_scales)
+        held = self.__dict__.get("_held")
+        if held is not None and held[0] == key and _same(tensors, held[1]):
+            return held[1]
+        ptrs = (_arg(self.k, pool, "k_pages", cache.page_dtype, device),
+                _arg(self.v, pool, "v_pages", cache.page_dtype, device),
+                _arg(self.k_scales, scales, "k_scales", torch.uint8, device),
+                _arg(self.v_scales, scales, "v_scales", torch.uint8, device))
+        self.__dict__["_held"] = (key, ptrs)
+        return ptrs
+
 
 def _arg_batch(cache: Cache, page_table, seq_lens, new_start, pages: Pages, device: int):
     """Pointers of page_table, seq_lens, new_start and the four pools."""
     b, i32 = cache.num_seqs, torch.int32
-    _, _, _, pool, scales = cache._sizes
     return (_arg(page_table, b * cache.table_width, "page_table", i32, device),
             _arg(seq_lens, b, "seq_lens", i32, device),
-            _arg(new_start, b + 1, "new_start", i32, device),
-            _arg(pages.k, pool, "k_pages", cache.page_dtype, device),
-            _arg(pages.v, pool, "v_pages", cache.page_dtype, device),
-            _arg(pages.k_scales, scales, "k_scales", torch.uint8, device),
-            _arg(pages.v_scales, scales, "v_scales", torch.uint8, device))
+            _arg(new_start, b + 1, "new_start", i32, device), *pages._args(cache, device))
 
 
 def proxyattn_cache_append(cache: Cache, rotary: Rotary | None, q, k, v, q_out, page_table,
@@ -714,14 +748,13 @@ def proxyattn_cache_append(cache: Cache, rotary: Rotary | None, q, k, v, q_out, 
     dev, st = _device_and_stream(stream)
     dt = cache.torch_dtype
     nq, nkv = cache._sizes[:2]
-    r = _arg_rotary(rotary, cache.head_dim, dt, dev)
+    r = rotary._arg(cache.head_dim, dt, dev) if rotary is not None else None
     out = _span(cache.num_tokens, cache.num_q_heads, cache.head_dim, rotary.q_out_tok_stride,
                 rotary.q_out_head_stride) if rotary is not None else 0
     args = (_arg(q, nq, "q", dt, dev, False), _arg(k, nkv, "k", dt, dev, False),
             _arg(v, nkv, "v", dt, dev, False), _arg(q_out, out, "q_out", dt, dev, False))
     batch = _arg_batch(cache, page_table, seq_lens, new_start, pages, dev)
-    _check(lib().proxyattn_cache_append(ctypes.byref(cache._c), r, *args, *batch,
-                                        st))
+    _check(lib().proxyattn_cache_append(cache._ref, r, *args, *batch, st))
 
 
 def proxyattn_cache_read(cache: Cache, page_table, seq_lens, new_start, pages: Pages, k_out,
@@ -731,7 +764,7 @@ def proxyattn_cache_read(cache: Cache, page_table, seq_lens, new_start, pages: P
     outs = (_arg(k_out, nkv, "k_out", cache.torch_dtype, dev, False),
             _arg(v_out, nkv, "v_out", cache.torch_dtype, dev, False))
     batch = _arg_batch(cache, page_table, seq_lens, new_start, pages, dev)
-    _check(lib().proxyattn_cache_read(ctypes.byref(cache._c), *batch, *outs, st))
+    _check(lib().proxyattn_cache_read(cache._ref, *batch, *outs, st))
 
 
 def proxyattn_cache_attention(cache: Cache, q, page_table, seq_lens, new_start, pages: Pages, out,
@@ -743,11 +776,16 @@ def proxyattn_cache_attention(cache: Cache, q, page_table, seq_lens, new_start, 
     batch = _arg_batch(cache, page_table, seq_lens, new_start, pages, dev)
     op = _arg(out, no, "out", dt, dev, False)
     lp = _arg(lse, cache.num_q_heads * cache.num_tokens, "lse", torch.float32, dev)
-    _need_ws(workspace, cache._workspace_bytes)
-    _check(lib().proxyattn_cache_attention(
-        ctypes.byref(cache._c), qp, *batch, op, lp, _ptr(workspace),
-        _nbytes(workspace) if isinstance(workspace, torch.Tensor) else
-        (0 if workspace is None else cache._workspace_bytes), st))
+    need = ws_bytes = cache._workspace_bytes
+    if isinstance(workspace, torch.Tensor):
+        ws_bytes = _nbytes(workspace)
+        if not (ws_bytes >= need and workspace.get_device() == dev >= 0 and workspace.is_contiguous()):
+            _need_ws(workspace, need)
+        workspace = workspace.data_ptr()
+    elif workspace is None:
+        ws_bytes = 0
+    _check(lib().proxyattn_cache_attention(cache._ref, qp, *batch, op, lp, workspace, ws_bytes,
+                                           st))
 
 
 def proxyattn_version() -> str:

@@ -106,17 +106,25 @@ def _call(lib, name, *args):
                                 for a in args])
 
 
-def test_workspace_of_cache_attention(lib):
-    """First units of every sequence, then two partial rows sets to a workgroup
-    (at most 512): reference and sum, and the output, each region rounded up to
-    256 bytes."""
+@pytest.mark.parametrize("kw,rows,groups", [
+    # 4 sequences x 8 heads, each 8 units of 128 keys and one for its start
+    ({}, 16, 288),
+    # 4 bits: units of 256 keys; 8 new tokens of 4 heads
+    (dict(cache_type="fp4", max_new=8, num_tokens=32), 32, 160),
+    # as many workgroups as two on each of 256 CUs, or one where the rows need the registers
+    (dict(num_seqs=64, num_tokens=64), 16, 512),
+    (dict(num_seqs=64, num_tokens=2000, max_new=100), 64, 256),
+    (dict(num_seqs=64, num_tokens=2000, max_new=100, dtype="fp32"), 32, 256),
+])
+def test_workspace_of_cache_attention(lib, kw, rows, groups):
+    """First units of every sequence, then two sets of partial rows to a
+    workgroup: reference and sum, and the output, each region rounded up to 256
+    bytes."""
     def up(x):
         return -(-x // 256) * 256
-    # 4 sequences x 8 heads x 8 units of 128 keys: 256 workgroups, 16 rows
-    assert pa.proxyattn_cache_workspace_size(_cache()) == 256 + up(512 * 16 * 8) + 512 * 16 * 512
-    # 4 bits: units of 256 keys; 8 new tokens of 4 heads: 32 rows
-    c = _cache(cache_type="fp4", max_new=8, num_tokens=32)
-    assert pa.proxyattn_cache_workspace_size(c) == 256 + up(256 * 32 * 8) + 256 * 32 * 512
+    c = _cache(**kw)
+    assert pa.proxyattn_cache_workspace_size(c) == (
+        up(4 * (c.num_seqs + 1)) + up(2 * groups * rows * 8) + 2 * groups * rows * 512)
 
 
 ARGS = {
