@@ -504,8 +504,8 @@ int proxyattn_cache_read(const proxyattn_cache* c, const int32_t* page_table,
  *     out[t][i] = softmax_u(c <q_t, k_u>) v_u,  lse[i][t] = log sum_u exp(c <q_t, k_u>).
  *  q: [T][Hq][d]; out: [T][Hq][d]; the cache's q and o strides.
  *  lse: [Hq][T] fp32, or NULL.
- *  workspace: at least proxyattn_cache_workspace_size bytes, 16-byte aligned;
- *      nothing in it outlasts the call.
+ *  workspace: at least proxyattn_cache_workspace_size bytes (which may be 0),
+ *      16-byte aligned; nothing in it outlasts the call.
  * Made for few new tokens a sequence: every 16 to 64 (token, head) rows of a KV
  * head read its cache once.  A whole prompt is the prefill calls' work.
  */

@@ -73,7 +73,7 @@ struct CacheWs {
     size_t total;
     int groups;    // workgroups W
     int tiles;     // 16-row tiles of a workgroup's rows: 1 to 4
-    int joined;    // whether a (sequence, head) can be split over workgroups
+    int joined;    // whether runs of units are cut between workgroups (else one to each)
 };
 // False: more units of work than an int counts.
 bool cache_ws(const CacheShape& s, CacheWs* w);

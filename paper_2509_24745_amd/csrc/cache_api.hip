@@ -331,7 +331,7 @@ int proxyattn_cache_attention(const proxyattn_cache* c, const void* q, const int
     PA_TRY(check_ptr(out, "out"));
     if (lse && ((uintptr_t)lse & 3u)) return fail(PROXYATTN_E_INVALID, "lse not 4-byte aligned");
     PA_TRY(check_batch(s, page_table, seq_lens, new_start, k_pages, v_pages, k_scales, v_scales));
-    PA_TRY(check_ptr(workspace, "workspace"));
+    if (w.total) PA_TRY(check_ptr(workspace, "workspace"));
     if (workspace_bytes < w.total)
         return fail(PROXYATTN_E_WORKSPACE, "workspace %zu bytes < %zu needed", workspace_bytes,
                     w.total);

@@ -58,6 +58,14 @@ constexpr int groups_per_cu(bool fp4, int esz, int d, int nr) {
 // before the run's first keys.
 constexpr int kStartUnits = 1;
 
+// Up to so many units a run is a workgroup's own, by the number of runs: one
+// launch, and nobody looks up who has what.  Calls in a graph, 32 query heads on 8,
+// d 128, whole against cut (us): 1 sequence (8 runs) of 512 keys in bf16 (4 units)
+// 8.6 / 9.2, of 1024 13.0 / 9.3; 8 sequences of 1024 13.9 / 16.2, 4 bits 2048 (8
+// units) 15.2 / 14.6; 64 of 1024 44.7 / 49.5.  Longer runs of many sequences gain
+// as much where their lengths are equal, but lose more where they are not.
+static int whole_units(int64_t runs) { return runs >= 64 ? 8 : 4; }
+
 // A sequence of the batch as the header reads its arrays.
 struct Seq {
     int len, row, fresh;   // cached tokens, first row, new tokens
@@ -528,7 +536,7 @@ template <typename T, bool FP4, int D, int NR, bool PAST>
 __global__ __launch_bounds__(kAttnThreads, groups_per_cu(FP4, sizeof(T), D, NR)) void
 cache_attn_kernel(
     CacheShape s, const T* qp, const int* table, const int* lens, const int* starts, PagePtrs pg,
-    T* out, float* lse, int* plan, float2* stat, float* part) {
+    T* out, float* lse, int max_tiles, int* plan, float2* stat, float* part) {
     typedef KeyStep<T, FP4, D> Keys;
     constexpr int KT = Keys::KT, SK = 16 * KT, UNIT = 4 * SK, ROWS = 16 * NR, OC = D / 16;
     constexpr int LINE = D + 4;   // a row's outputs in LDS, padded by a bank group
@@ -539,31 +547,49 @@ cache_attn_kernel(
     const int g = lane >> 4, n = lane & 15;
     const int group = blockIdx.x;
 
+    auto uniform = [](Seq q) {
+        return Seq{wave_uniform(q.len), wave_uniform(q.row), wave_uniform(q.fresh)};
+    };
     __shared__ Seq seqs[kAttnThreads];
-    const Found found = find_unit<ROWS, UNIT>(s, lens, starts, group == 0 ? plan : nullptr,
-                                              gridDim.x, group, seqs);
-    int b = found.b, base = found.base;
-    int f = found.begin;
+    const bool own = !plan;   // a workgroup to a run
+    Found found = {0, 1, 0, 0};
+    if (own)
+        found.b = group / (s.hkv * max_tiles);
+    else
+        found = find_unit<ROWS, UNIT>(s, lens, starts, group == 0 ? plan : nullptr, gridDim.x,
+                                      group, seqs);
+    int f = found.begin, b = found.b, base = found.base;
     while (f < found.end) {
-        Seq sq = s.b <= kAttnThreads ? seqs[b] : seq_at(s, lens, starts, b);
-        sq.len = wave_uniform(sq.len);
-        sq.row = wave_uniform(sq.row);
-        sq.fresh = wave_uniform(sq.fresh);
+        const Seq sq = uniform(!own && s.b <= kAttnThreads ? seqs[b] : seq_at(s, lens, starts, b));
         const Runs<ROWS, UNIT> run(s, sq);
-        const int past = base + s.hkv * run.tiles * run.flat();
-        if (f >= past) {   // on to the next sequence
-            base = past;
-            ++b;
-            continue;
+        // units u0 .. u1 - 1 of a run; if these are not all, partial rows go to slot
+        int head, row0, u0, u1, slot = 0;
+        if (own) {
+            const int item = group - b * s.hkv * max_tiles;
+            head = item / max_tiles;
+            row0 = (item - head * max_tiles) * ROWS;
+            u0 = 0;
+            u1 = run.units;
+            f = 1;
+            if (row0 >= run.tiles * ROWS) break;
+        } else {
+            const int past = base + s.hkv * run.tiles * run.flat();
+            if (f >= past) {   // on to the next sequence
+                base = past;
+                ++b;
+                continue;
+            }
+            const int at = f - base, item = at / run.flat(), u = at - item * run.flat();
+            const int ahead = min(run.flat(), u + (found.end - f));
+            head = item / run.tiles;
+            row0 = (item - head * run.tiles) * ROWS;
+            u0 = max(u - kStartUnits, 0);
+            u1 = ahead - kStartUnits;
+            // a run that goes on from the workgroup before, or starts here
+            slot = 2 * group + (f - u + kStartUnits > found.begin ? 1 : 0);
+            f += ahead - u;
+            if (u1 <= 0) continue;
         }
-        const int at = f - base, item = at / run.flat(), u = at - item * run.flat();
-        const int ahead = min(run.flat(), u + (found.end - f));
-        const int head = item / run.tiles, row0 = (item - head * run.tiles) * ROWS;
-        const int u0 = max(u - kStartUnits, 0), u1 = ahead - kStartUnits;
-        // a run that goes on from the workgroup before, or starts here
-        const int slot = 2 * group + (f - u + kStartUnits > found.begin ? 1 : 0);
-        f += ahead - u;
-        if (u1 <= 0) continue;
 
         // rows: (new token, query head of the KV head); row n of tile nr sees keys up to limit
         const int rows = sq.fresh * s.rep, newest = sq.len - sq.fresh;
@@ -813,8 +839,13 @@ bool cache_ws(const CacheShape& s, CacheWs* w) {
     const int64_t runs = (int64_t)s.b * s.hkv * max_row_tiles(s, w->tiles);
     // a workgroup of 256 threads to each run in the second launch
     if (rows > INT32_MAX || runs > INT32_MAX / 256 || runs * flat > INT32_MAX) return false;
+    w->joined = units > whole_units(runs);
+    if (!w->joined) {
+        w->groups = (int)runs;
+        w->total = 0;
+        return true;
+    }
     w->groups = (int)std::max<int64_t>(1, std::min<int64_t>(kCus * groups_per_cu(s.fp4, esz, s.d, w->tiles), runs * flat));
-    w->joined = units > 1;
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     const size_t parts = (size_t)2 * w->groups * 16 * w->tiles;
     size_t off = 0;
@@ -829,18 +860,18 @@ template <typename T, int D, bool FP4, int NR>
 static void attention_as(const CacheShape& s, const void* q, const int* table, const int* lens,
                          const int* starts, const PagePtrs& pg, void* out, float* lse, char* ws,
                          const CacheWs& w, hipStream_t st) {
-    int* plan = (int*)(ws + w.plan);
+    const int mt = max_row_tiles(s, NR);
+    int* plan = w.joined ? (int*)(ws + w.plan) : nullptr;
     float2* stat = (float2*)(ws + w.stat);
     float* part = (float*)(ws + w.part);
     if (s.past)
         cache_attn_kernel<T, FP4, D, NR, true><<<w.groups, kAttnThreads, 0, st>>>(
-            s, (const T*)q, table, lens, starts, pg, (T*)out, lse, plan, stat, part);
+            s, (const T*)q, table, lens, starts, pg, (T*)out, lse, mt, plan, stat, part);
     else
         cache_attn_kernel<T, FP4, D, NR, false><<<w.groups, kAttnThreads, 0, st>>>(
-            s, (const T*)q, table, lens, starts, pg, (T*)out, lse, plan, stat, part);
+            s, (const T*)q, table, lens, starts, pg, (T*)out, lse, mt, plan, stat, part);
     if (!w.joined) return;
     constexpr int UNIT = 64 * key_tiles(FP4, sizeof(T), D);
-    const int mt = max_row_tiles(s, NR);
     const int rows = std::min(16 * NR, s.rep * s.max_new);
     const dim3 grid((unsigned)s.b * s.hkv * mt, rows);
     cache_join_kernel<T, D, NR, UNIT><<<grid, 256, 0, st>>>(s, lens, starts, mt, w.groups, plan,

@@ -69,7 +69,7 @@ def _cache(**kw):
 def test_cache_validation(lib, kw, code):
     c = _cache(**kw)
     if code is None:
-        assert pa.proxyattn_cache_workspace_size(c) > 0
+        assert pa.proxyattn_cache_workspace_size(c) >= 0
         return
     with pytest.raises(pa.ProxyAttnError) as ei:
         pa.proxyattn_cache_workspace_size(c)
@@ -110,11 +110,14 @@ def _call(lib, name, *args):
     # 4 sequences x 8 heads, each 8 units of 128 keys and one for its start
     ({}, 16, 288),
     # 4 bits: units of 256 keys; 8 new tokens of 4 heads
-    (dict(cache_type="fp4", max_new=8, num_tokens=32), 32, 160),
+    (dict(cache_type="fp4", max_new=8, num_tokens=32, table_width=32, max_len=2000), 32, 288),
+    # at most 4 units, or 8 of 64 runs: a workgroup to each run, no workspace
+    (dict(cache_type="fp4"), 0, 0), (dict(num_seqs=8, num_tokens=8), 0, 0),
     # as many workgroups as two on each of 256 CUs, or one where the rows need the registers
-    (dict(num_seqs=64, num_tokens=64), 16, 512),
-    (dict(num_seqs=64, num_tokens=2000, max_new=100), 64, 256),
-    (dict(num_seqs=64, num_tokens=2000, max_new=100, dtype="fp32"), 32, 256),
+    (dict(num_seqs=64, num_tokens=64, max_len=1025, table_width=17), 16, 512),
+    (dict(num_seqs=64, num_tokens=2000, max_new=100, max_len=1025, table_width=17), 64, 256),
+    (dict(num_seqs=64, num_tokens=2000, max_new=100, max_len=1025, table_width=17,
+          dtype="fp32"), 32, 256),
 ])
 def test_workspace_of_cache_attention(lib, kw, rows, groups):
     """First units of every sequence, then two sets of partial rows to a
@@ -123,6 +126,9 @@ def test_workspace_of_cache_attention(lib, kw, rows, groups):
     def up(x):
         return -(-x // 256) * 256
     c = _cache(**kw)
+    if not groups:
+        assert pa.proxyattn_cache_workspace_size(c) == 0
+        return
     assert pa.proxyattn_cache_workspace_size(c) == (
         up(4 * (c.num_seqs + 1)) + up(2 * groups * rows * 8) + 2 * groups * rows * 512)
 
