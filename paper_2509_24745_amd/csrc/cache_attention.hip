@@ -34,7 +34,7 @@
 namespace pa {
 
 constexpr int kAttnThreads = 256;   // 4 waves
-constexpr int kCus = 256;
+constexpr int kCus = 256, kCuShift = 8;
 constexpr int kCacheGroups = 2 * kCus;   // workgroups at most
 // Below any score that a finite row gives: the reference before the first key.
 constexpr float kNoScore = -1e30f;
@@ -100,11 +100,16 @@ struct Found {
     int begin, end, b, base;   // the workgroup's units; the sequence that begin lies in
 };
 // Workgroup w's first unit of `total`, and the workgroup that unit f is with.
+// Fewer than kCus or twice kCus workgroups are as many as there can be units,
+// and have one each (or none).
 __device__ __forceinline__ int first_unit(int total, int groups, int w) {
-    return (int)((int64_t)w * total / groups);
+    if (total <= groups) return min(w, total);
+    return (int)((int64_t)w * total >> (groups == kCus ? kCuShift : kCuShift + 1));
 }
 __device__ __forceinline__ int group_of(int total, int groups, int f) {
-    return (int)((((int64_t)f + 1) * groups - 1) / total);
+    if (total <= groups) return f;
+    // in doubles: the quotient is at least 1 / total off every whole number above it
+    return (int)((((double)f + 1) * groups - 1) / total);
 }
 template <int ROWS, int UNIT>
 __device__ __forceinline__ Found find_unit(const CacheShape& s, const int* lens, const int* starts,
@@ -138,10 +143,7 @@ __device__ __forceinline__ Found find_unit(const CacheShape& s, const int* lens,
         if (w < wave) before += wave_total[w];
         all += wave_total[w];
     }
-    groups = min(groups, all);   // a unit at least to each that has any
-    const bool any = group < groups;
-    const int want = any ? first_unit(all, groups, group) : all;
-    const int end = any ? first_unit(all, groups, group + 1) : all;
+    const int want = first_unit(all, groups, group), end = first_unit(all, groups, group + 1);
     if (plan || (want >= before && want < before + mine)) {
         int at = before;
         for (int b = b0; b < b1; ++b) {
@@ -156,6 +158,7 @@ __device__ __forceinline__ Found find_unit(const CacheShape& s, const int* lens,
     }
     if (plan && tid == 0) plan[s.b] = all;
     __syncthreads();
+    const bool any = want < end;
     return {want, end, any ? wave_uniform(found[0]) : 0, any ? wave_uniform(found[1]) : 0};
 }
 
@@ -581,7 +584,7 @@ cache_attn_kernel(
             }
             const int at = f - base, item = at / run.flat(), u = at - item * run.flat();
             const int ahead = min(run.flat(), u + (found.end - f));
-            head = item / run.tiles;
+            head = run.tiles == 1 ? item : item / run.tiles;
             row0 = (item - head * run.tiles) * ROWS;
             u0 = max(u - kStartUnits, 0);
             u1 = ahead - kStartUnits;
@@ -593,11 +596,12 @@ cache_attn_kernel(
 
         // rows: (new token, query head of the KV head); row n of tile nr sees keys up to limit
         const int rows = sq.fresh * s.rep, newest = sq.len - sq.fresh;
+        auto token_of = [&](int row) { return sq.fresh == 1 ? 0 : row / s.rep; };
         Rows<T, FP4, D, NR> r;
         int limit[NR];
         float ref[NR], sum[NR];
         r.q.load(queries, lane, [&](int i) -> const T* {
-            const int row = row0 + i, j = row / s.rep;
+            const int row = row0 + i, j = token_of(row);
             return row < rows ? qp + (int64_t)(sq.row + j) * s.q_tok +
                                     (int64_t)(head * s.rep + row - j * s.rep) * s.q_head
                               : nullptr;
@@ -605,14 +609,14 @@ cache_attn_kernel(
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr) {
             const int row = row0 + 16 * nr + n;
-            limit[nr] = row < rows ? newest + row / s.rep : sq.len - 1;
+            limit[nr] = row < rows ? newest + token_of(row) : sq.len - 1;
             ref[nr] = kNoScore;
             sum[nr] = 0.f;
 #pragma unroll
             for (int i = 0; i < OC; ++i) r.o[nr][i] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        const int all_see = newest + row0 / s.rep;   // keys up to here: every row
-        const int some_see = newest + (min(row0 + ROWS, rows) - 1) / s.rep;
+        const int all_see = newest + token_of(row0);   // keys up to here: every row
+        const int some_see = newest + token_of(min(row0 + ROWS, rows) - 1);
         const int key0 = u0 * UNIT, key1 = min(u1 * UNIT, some_see + 1);
 
         // page of a step's keys for this lane, inside the sequence
@@ -730,7 +734,7 @@ cache_attn_kernel(
                     for (int j = 0; j < 8; ++j) z[j] += m[j];
                 }
                 if (whole) {
-                    const int j = row / s.rep;
+                    const int j = token_of(row);
                     const int64_t t = sq.row + j, i = head * s.rep + row - j * s.rep;
                     const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
@@ -770,7 +774,6 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheShape s, const int
     const int head = item / max_tiles, tile = item - head * max_tiles;
     const Seq sq = seq_at(s, lens, starts, b);
     const int total = plan[s.b], base = plan[b];
-    groups = min(groups, total);
     const Runs<ROWS, UNIT> run(s, sq);
     const int row = tile * ROWS + line;
     if (tile >= run.tiles || row >= sq.fresh * s.rep) return;
