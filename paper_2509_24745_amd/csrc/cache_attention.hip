@@ -25,6 +25,7 @@
 // 17/16 D in 4 bits, for 4 D products a row; at 16 rows that is 16 and 60
 // products a byte, where the card's rates balance at 250.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.h"
 #include "cache_device.h"
@@ -55,8 +56,10 @@ constexpr int groups_per_cu(bool fp4, int esz, int d, int nr) {
 
 // Units that a run's start counts for when the work is dealt: a workgroup's
 // time goes by the runs it starts as well as by the keys it reads.  They lie
-// before the run's first keys.
-constexpr int kStartUnits = 1;
+// before the run's first keys.  With 0, 1, 2, 3 and 4 of them (us): 64 sequences of up to
+// 32K tokens in 4 bits 44.7, 37.1, 36.0, 37.4, 37.2; 64 to 8K in bf16 -, 87.8, 88.7, 92.7,
+// 94.7, 4 to 24K with 9 new tokens 47.1, 45.2, 43.1, 41.1, 43.4.
+constexpr int start_units(bool fp4, int nr) { return fp4 ? 2 : nr == 1 ? 1 : 3; }
 
 // Up to so many units a run is a workgroup's own, by the number of runs: one
 // launch, and nobody looks up who has what.  Calls in a graph, 32 query heads on 8,
@@ -84,11 +87,11 @@ __device__ __forceinline__ Seq seq_at(const CacheShape& s, const int* lens, cons
 }
 
 // Row tiles of a KV head and units of a row tile.
-template <int ROWS, int UNIT> struct Runs {
+template <int ROWS, int UNIT, int START> struct Runs {
     int tiles, units;
     __device__ __forceinline__ Runs(const CacheShape& s, const Seq& q)
         : tiles((q.fresh * s.rep + ROWS - 1) / ROWS), units(max(1, (q.len + UNIT - 1) / UNIT)) {}
-    __device__ __forceinline__ int flat() const { return units + kStartUnits; }
+    __device__ __forceinline__ int flat() const { return units + START; }
 };
 
 __device__ __forceinline__ int wave_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -111,7 +114,7 @@ __device__ __forceinline__ int group_of(int total, int groups, int f) {
     // in doubles: the quotient is at least 1 / total off every whole number above it
     return (int)((((double)f + 1) * groups - 1) / total);
 }
-template <int ROWS, int UNIT>
+template <int ROWS, int UNIT, int START>
 __device__ __forceinline__ Found find_unit(const CacheShape& s, const int* lens, const int* starts,
                                            int* plan, int groups, int group, Seq* seqs) {
     __shared__ int wave_total[4];
@@ -120,7 +123,7 @@ __device__ __forceinline__ Found find_unit(const CacheShape& s, const int* lens,
     const int chunk = (s.b + kAttnThreads - 1) / kAttnThreads;
     const int b0 = min(tid * chunk, s.b), b1 = min(b0 + chunk, s.b);
     auto count = [&](const Seq& q) {
-        const Runs<ROWS, UNIT> r(s, q);
+        const Runs<ROWS, UNIT, START> r(s, q);
         return s.hkv * r.tiles * r.flat();
     };
     int mine = 0;
@@ -308,62 +311,105 @@ __device__ __forceinline__ uint32_t fp4_pair_bf16(uint32_t w, float scale, int b
 }
 __device__ __forceinline__ bf16x8 as_frag(const u32x4& w) { return __builtin_bit_cast(bf16x8, w); }
 
-// The queries of NR tiles of 16 rows.  Piece i of a row for lane group g is the
-// values that the group's part of a key holds.  One tile's stay in registers; several
-// tiles' lie in LDS, lines padded by 16 bytes so that 16 rows meet all banks, and
-// are read in every step: the registers hold the outputs and the next keys.
+// fp32 values as TERMS bf16 values that add up to them: each the rounding of
+// what those before leave (three hold all 24 bits).
+template <int TERMS>
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t (&w)[TERMS]) {
+#pragma unroll
+    for (int i = 0; i < TERMS; ++i) {
+        w[i] = pack_rne(a, b);
+        if (i + 1 < TERMS) {
+            a -= __uint_as_float(w[i] << 16);
+            b -= __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+}
+
+// The queries of NR tiles of 16 rows, as 16-byte pieces for the MFMAs.  Piece i
+// of a row for lane group g is what meets the group's part of a key.  Queries in fp32
+// over 4-bit keys, which are bf16 values, go as three bf16 terms of 8 values, else a
+// piece holds values as they are.  One tile's pieces stay in registers; several
+// tiles' lie in LDS, lines padded by 16 bytes so that 16 rows meet all banks, and are
+// read in every step: the registers hold the outputs and the next keys.
 template <typename T, bool FP4, int D, int NR> struct Queries {
-    static constexpr int N = 16 / sizeof(T), QC = D / 4 / N;   // pieces of 16 bytes
-    static constexpr int LINE = D + N;
+    static constexpr int TERMS = FP4 && sizeof(T) == 4 ? 3 : 1;
+    typedef typename std::conditional<TERMS == 3, bf16, T>::type E;
+    static constexpr int N = 16 / sizeof(E), QC = D / 4 / N;   // pieces of a term
+    static constexpr int LINE = TERMS * D + N;
     static constexpr int LDS = NR == 1 ? 4 : 16 * NR * LINE;   // elements
     static constexpr bool kept = NR == 1;
     static __device__ __forceinline__ int piece_at(int i, int g) {
         return FP4 ? D / 4 * g + N * i : 4 * N * i + N * g;
     }
-    u32x4 reg[kept ? QC : 1];
-    const T* lds;
+    u32x4 reg[kept ? TERMS * QC : 1];
+    const E* lds;
 
+    // N values of a row as their terms
+    static __device__ __forceinline__ void terms(const T* p, u32x4 (&w)[TERMS]) {
+        if constexpr (TERMS == 1) {
+            w[0] = *reinterpret_cast<const u32x4*>(p);
+        } else {
+            const f32x4 x[2] = {*reinterpret_cast<const f32x4*>(p),
+                                *reinterpret_cast<const f32x4*>(p + 4)};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t z[TERMS];
+                split_pair(x[j / 2][2 * (j % 2)], x[j / 2][2 * (j % 2) + 1], z);
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) w[k][j] = z[k];
+            }
+        }
+    }
     // row(n): row n of the tiles, or NULL for none
-    template <typename F> __device__ __forceinline__ void load(T* buf, int lane, F row) {
+    template <typename F> __device__ __forceinline__ void load(E* buf, int lane, F row) {
         lds = buf;
         if constexpr (kept) {
             const T* p = row(lane & 15);
 #pragma unroll
             for (int i = 0; i < QC; ++i) {
-                reg[i] = zero_u32x4();
-                if (p) reg[i] = *reinterpret_cast<const u32x4*>(p + piece_at(i, lane >> 4));
+                u32x4 w[TERMS];
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) w[k] = zero_u32x4();
+                if (p) terms(p + piece_at(i, lane >> 4), w);
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) reg[k * QC + i] = w[k];
             }
         } else {
             for (int x = threadIdx.x; x < 16 * NR * (D / N); x += kAttnThreads) {
                 const int n = x / (D / N), c = x % (D / N);
                 const T* p = row(n);
-                u32x4 w = zero_u32x4();
-                if (p) w = *reinterpret_cast<const u32x4*>(p + N * c);
-                *reinterpret_cast<u32x4*>(buf + n * LINE + N * c) = w;
+                u32x4 w[TERMS];
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) w[k] = zero_u32x4();
+                if (p) terms(p + N * c, w);
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k)
+                    *reinterpret_cast<u32x4*>(buf + n * LINE + k * D + N * c) = w[k];
             }
             __syncthreads();
         }
     }
-    __device__ __forceinline__ u32x4 piece(int nr, int i, int lane) const {
-        if constexpr (kept) return reg[i];
-        return *reinterpret_cast<const u32x4*>(lds + (16 * nr + (lane & 15)) * LINE +
+    __device__ __forceinline__ u32x4 piece(int nr, int i, int lane, int term = 0) const {
+        if constexpr (kept) return reg[term * QC + i];
+        return *reinterpret_cast<const u32x4*>(lds + (16 * nr + (lane & 15)) * LINE + term * D +
                                                piece_at(i, lane >> 4));
     }
 };
 
-// The rows' side of the products for NR tiles of 16 rows, and a step.
-template <typename T, bool FP4, int D, int NR> struct Rows;
-
-// bf16: MFMAs of 32 products.  For the scores, product i of lane group g takes
-// the values that chunk i of KeyStep holds; for the outputs, product (u, i)
-// takes the keys of tiles 2 u and 2 u + 1 and value D/16 m + i of row m, and two of
-// them: the probabilities as a bf16 and the bf16 of what that rounds off, so
-// that the output's own rounding is the only one that shows.  The second products
-// wait beside the loads.
-template <bool FP4, int D, int NR> struct Rows<bf16, FP4, D, NR> {
-    typedef KeyStep<bf16, FP4, D> Keys;
-    static constexpr int KT = Keys::KT, QC = D / 32, OC = D / 16;
-    Queries<bf16, FP4, D, NR> q;
+// The rows' side of the products for NR tiles of 16 rows, and a step.  Keys and
+// values that are bf16 values: MFMAs of 32 products.  For the scores, product i of
+// lane group g takes the values that chunk i of KeyStep holds; for the outputs,
+// product (u, i) takes the keys of tiles 2 u and 2 u + 1 and value D/16 m + i of row m.
+// Probabilities go as a bf16 and the bf16 of what that rounds off, so that the
+// output's own rounding is the only one that shows (with the one bf16, its errors
+// are 1.4 times as large; 10 % of the time of 64 rows, none of 16, where the MFMAs
+// wait beside the loads).  fp32 rows take three terms of the queries and of the
+// probabilities: exact products as with fp32 MFMAs, in a fifth of their cycles.
+template <typename T, bool FP4, int D, int NR> struct Rows {
+    typedef KeyStep<T, FP4, D> Keys;
+    typedef Queries<T, FP4, D, NR> Q;
+    static constexpr int KT = Keys::KT, QC = D / 32, OC = D / 16, PT = Q::TERMS == 3 ? 3 : 2;
+    Q q;
     f32x4 o[NR][OC];
 
     __device__ __forceinline__ void scores(const Keys& ks, int lane, f32x4 (&x)[NR][KT]) const {
@@ -390,12 +436,14 @@ template <bool FP4, int D, int NR> struct Rows<bf16, FP4, D, NR> {
 #pragma unroll
                 for (int t = 0; t < 2; ++t) x[nr][t0 + t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < QC; ++i) {
-                    const bf16x8 qf = as_frag(q.piece(nr, i, lane));
+                for (int k = Q::TERMS - 1; k >= 0; --k)   // smallest first
 #pragma unroll
-                    for (int t = 0; t < 2; ++t)
-                        x[nr][t0 + t] = mma16(kf[t][i], qf, x[nr][t0 + t]);
-                }
+                    for (int i = 0; i < QC; ++i) {
+                        const bf16x8 qf = as_frag(q.piece(nr, i, lane, k));
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+                            x[nr][t0 + t] = mma16(kf[t][i], qf, x[nr][t0 + t]);
+                    }
             }
         }
     }
@@ -403,20 +451,20 @@ template <bool FP4, int D, int NR> struct Rows<bf16, FP4, D, NR> {
 #pragma unroll
         for (int u = 0; u < KT / 2; ++u) {
             if constexpr (NR > 1) __builtin_amdgcn_sched_barrier(0);
-            bf16x8 hi[NR], lo[NR];
+            bf16x8 pf[NR][PT];
 #pragma unroll
             for (int nr = 0; nr < NR; ++nr) {
-                u32x4 h, l;
+                u32x4 f[PT];
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const float a = p[nr][2 * u + w / 2][2 * (w % 2)];
-                    const float b = p[nr][2 * u + w / 2][2 * (w % 2) + 1];
-                    h[w] = pack_rne(a, b);
-                    l[w] = pack_rne(a - __uint_as_float(h[w] << 16),
-                                    b - __uint_as_float(h[w] & 0xffff0000u));
+                    uint32_t z[PT];
+                    split_pair(p[nr][2 * u + w / 2][2 * (w % 2)],
+                               p[nr][2 * u + w / 2][2 * (w % 2) + 1], z);
+#pragma unroll
+                    for (int k = 0; k < PT; ++k) f[k][w] = z[k];
                 }
-                hi[nr] = as_frag(h);
-                lo[nr] = as_frag(l);
+#pragma unroll
+                for (int k = 0; k < PT; ++k) pf[nr][k] = as_frag(f[k]);
             }
             if constexpr (NR > 2) __builtin_amdgcn_sched_barrier(0);
             // slots 2 w, 2 w + 1 of the fragment: keys KT r + 2 u + w / 2, r = 2 (w % 2) and the next
@@ -438,24 +486,24 @@ template <bool FP4, int D, int NR> struct Rows<bf16, FP4, D, NR> {
                     odd[w] = __builtin_amdgcn_perm(b, a, 0x07060302u);
                 }
 #pragma unroll
-                for (int nr = 0; nr < NR; ++nr) {
-                    o[nr][2 * c] = mma16(as_frag(even), hi[nr], o[nr][2 * c]);
-                    o[nr][2 * c + 1] = mma16(as_frag(odd), hi[nr], o[nr][2 * c + 1]);
-                    o[nr][2 * c] = mma16(as_frag(even), lo[nr], o[nr][2 * c]);
-                    o[nr][2 * c + 1] = mma16(as_frag(odd), lo[nr], o[nr][2 * c + 1]);
-                }
+                for (int k = PT - 1; k >= 0; --k)
+#pragma unroll
+                    for (int nr = 0; nr < NR; ++nr) {
+                        o[nr][2 * c] = mma16(as_frag(even), pf[nr][k], o[nr][2 * c]);
+                        o[nr][2 * c + 1] = mma16(as_frag(odd), pf[nr][k], o[nr][2 * c + 1]);
+                    }
             }
         }
     }
 };
 
-// fp32: MFMAs of 4 products, one value of each lane group, exact as fp32
-// products are.  Their rate, 1/16 of bf16's, still outruns the cache's bytes
+// fp32 keys and values: MFMAs of 4 products, one value of each lane group, exact as
+// fp32 products are.  Their rate, 1/16 of bf16's, still outruns the cache's bytes
 // four times.
-template <bool FP4, int D, int NR> struct Rows<float, FP4, D, NR> {
-    typedef KeyStep<float, FP4, D> Keys;
+template <int D, int NR> struct Rows<float, false, D, NR> {
+    typedef KeyStep<float, false, D> Keys;
     static constexpr int KT = Keys::KT, QC = D / 16, OC = D / 16;
-    Queries<float, FP4, D, NR> q;
+    Queries<float, false, D, NR> q;
     f32x4 o[NR][OC];
 
     __device__ __forceinline__ void scores(const Keys& ks, int lane, f32x4 (&x)[NR][KT]) const {
@@ -464,28 +512,19 @@ template <bool FP4, int D, int NR> struct Rows<float, FP4, D, NR> {
 #pragma unroll
             for (int t = 0; t < KT; ++t) x[nr][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < QC; i += 2) {
+        for (int i = 0; i < QC; ++i) {
             if constexpr (NR > 1) __builtin_amdgcn_sched_barrier(0);
-            u32x4 qf[NR][2];
+            u32x4 qf[NR];
 #pragma unroll
-            for (int nr = 0; nr < NR; ++nr)
+            for (int nr = 0; nr < NR; ++nr) qf[nr] = q.piece(nr, i, lane);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) qf[nr][j] = q.piece(nr, i + j, lane);
+            for (int t = 0; t < KT; ++t)
 #pragma unroll
-            for (int t = 0; t < KT; ++t) {
-                float kf[8];
-                if constexpr (FP4) {
-                    fp4_values(ks.k[t][i / 2], ks.kscale(t), kf);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) kf[j] = __uint_as_float(ks.k[t][i + j / 4][j % 4]);
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
+                for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int nr = 0; nr < NR; ++nr)
-                        x[nr][t] = mma16(kf[j], __uint_as_float(qf[nr][j / 4][j % 4]), x[nr][t]);
-            }
+                        x[nr][t] = mma16(__uint_as_float(ks.k[t][i][j]), __uint_as_float(qf[nr][j]),
+                                         x[nr][t]);
         }
     }
     __device__ __forceinline__ void outputs(const Keys& ks, const f32x4 (&p)[NR][KT]) {
@@ -495,20 +534,11 @@ template <bool FP4, int D, int NR> struct Rows<float, FP4, D, NR> {
             for (int r = 0; r < 4; ++r) {
                 if constexpr (NR > 1) __builtin_amdgcn_sched_barrier(0);
                 const int x = KT * r + t;
-                float vf[OC];
-                if constexpr (FP4) {
-                    float z[8];
-                    fp4_values(ks.v[x], ks.vscale(x), z);
-#pragma unroll
-                    for (int i = 0; i < OC; ++i) vf[i] = z[i];
-                } else {
-#pragma unroll
-                    for (int i = 0; i < OC; ++i) vf[i] = __uint_as_float(ks.v[x][i]);
-                }
 #pragma unroll
                 for (int i = 0; i < OC; ++i)
 #pragma unroll
-                    for (int nr = 0; nr < NR; ++nr) o[nr][i] = mma16(vf[i], p[nr][t][r], o[nr][i]);
+                    for (int nr = 0; nr < NR; ++nr)
+                        o[nr][i] = mma16(__uint_as_float(ks.v[x][i]), p[nr][t][r], o[nr][i]);
             }
     }
 };
@@ -542,10 +572,11 @@ cache_attn_kernel(
     T* out, float* lse, int max_tiles, int* plan, float2* stat, float* part) {
     typedef KeyStep<T, FP4, D> Keys;
     constexpr int KT = Keys::KT, SK = 16 * KT, UNIT = 4 * SK, ROWS = 16 * NR, OC = D / 16;
+    constexpr int START = start_units(FP4, NR);
     constexpr int LINE = D + 4;   // a row's outputs in LDS, padded by a bank group
     __shared__ __align__(16) float merge[4][16][LINE];
     __shared__ float2 wstat[4][ROWS];
-    __shared__ __align__(16) T queries[Queries<T, FP4, D, NR>::LDS];
+    __shared__ __align__(16) typename Queries<T, FP4, D, NR>::E queries[Queries<T, FP4, D, NR>::LDS];
     const int lane = threadIdx.x & 63, wave = wave_uniform(threadIdx.x >> 6);
     const int g = lane >> 4, n = lane & 15;
     const int group = blockIdx.x;
@@ -559,12 +590,12 @@ cache_attn_kernel(
     if (own)
         found.b = group / (s.hkv * max_tiles);
     else
-        found = find_unit<ROWS, UNIT>(s, lens, starts, group == 0 ? plan : nullptr, gridDim.x,
+        found = find_unit<ROWS, UNIT, START>(s, lens, starts, group == 0 ? plan : nullptr, gridDim.x,
                                       group, seqs);
     int f = found.begin, b = found.b, base = found.base;
     while (f < found.end) {
         const Seq sq = uniform(!own && s.b <= kAttnThreads ? seqs[b] : seq_at(s, lens, starts, b));
-        const Runs<ROWS, UNIT> run(s, sq);
+        const Runs<ROWS, UNIT, START> run(s, sq);
         // units u0 .. u1 - 1 of a run; if these are not all, partial rows go to slot
         int head, row0, u0, u1, slot = 0;
         if (own) {
@@ -586,10 +617,10 @@ cache_attn_kernel(
             const int ahead = min(run.flat(), u + (found.end - f));
             head = run.tiles == 1 ? item : item / run.tiles;
             row0 = (item - head * run.tiles) * ROWS;
-            u0 = max(u - kStartUnits, 0);
-            u1 = ahead - kStartUnits;
+            u0 = max(u - START, 0);
+            u1 = ahead - START;
             // a run that goes on from the workgroup before, or starts here
-            slot = 2 * group + (f - u + kStartUnits > found.begin ? 1 : 0);
+            slot = 2 * group + (f - u + START > found.begin ? 1 : 0);
             f += ahead - u;
             if (u1 <= 0) continue;
         }
@@ -631,19 +662,23 @@ cache_attn_kernel(
             f32x4 x[NR][KT];
             r.scores(ks, lane, x);
             if (s0 + SK > sq.len) ks.drop_values(sq.len - (s0 + 4 * KT * g));
-            const bool ends = s0 + SK - 1 > all_see;
+            if (s0 + SK - 1 > all_see) {   // some row does not see all of the step
+#pragma unroll
+                for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+                    for (int t = 0; t < KT; ++t)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            if (s0 + KT * (4 * g + c) + t > limit[nr]) x[nr][t][c] = kNegInf;
+            }
 #pragma unroll
             for (int nr = 0; nr < NR; ++nr) {
-                float top = kNegInf;
+                float top = x[nr][0][0];
 #pragma unroll
                 for (int t = 0; t < KT; ++t)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float y = x[nr][t][c] * s.scale2;
-                        if (ends && s0 + KT * (4 * g + c) + t > limit[nr]) y = kNegInf;
-                        x[nr][t][c] = y;
-                        top = fmaxf(top, y);
-                    }
+                    for (int c = 0; c < 4; ++c) top = fmaxf(top, x[nr][t][c]);
+                top *= s.scale2;
                 if (__any(top > ref[nr] + kSlack)) {
                     const float next = fmaxf(ref[nr], groups_max(top));
                     const float shrink = fast_exp2(ref[nr] - next);
@@ -653,13 +688,12 @@ cache_attn_kernel(
                     for (int i = 0; i < OC; ++i) r.o[nr][i] *= shrink;
                 }
 #pragma unroll
-                for (int t = 0; t < KT; ++t)
+                for (int t = 0; t < KT; ++t) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const float p = fast_exp2(x[nr][t][c] - ref[nr]);
-                        x[nr][t][c] = p;
-                        sum[nr] += p;
-                    }
+                    for (int c = 0; c < 4; ++c)
+                        x[nr][t][c] = fast_exp2(fmaf(x[nr][t][c], s.scale2, -ref[nr]));
+                    sum[nr] += (x[nr][t][0] + x[nr][t][1]) + (x[nr][t][2] + x[nr][t][3]);
+                }
             }
             r.outputs(ks, x);
         };
@@ -757,7 +791,7 @@ cache_attn_kernel(
 // blockIdx.y of it.  D/4 threads hold a partial row, 256 / (D/4) partial rows
 // are read side by side, the first four of each before anything is known of
 // their references.
-template <typename T, int D, int NR, int UNIT>
+template <typename T, int D, int NR, int UNIT, int START>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheShape s, const int* lens,
                                                          const int* starts, int max_tiles,
                                                          int groups, const int* plan,
@@ -774,10 +808,10 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheShape s, const int
     const int head = item / max_tiles, tile = item - head * max_tiles;
     const Seq sq = seq_at(s, lens, starts, b);
     const int total = plan[s.b], base = plan[b];
-    const Runs<ROWS, UNIT> run(s, sq);
+    const Runs<ROWS, UNIT, START> run(s, sq);
     const int row = tile * ROWS + line;
     if (tile >= run.tiles || row >= sq.fresh * s.rep) return;
-    const int f0 = base + (head * run.tiles + tile) * run.flat() + kStartUnits;
+    const int f0 = base + (head * run.tiles + tile) * run.flat() + START;
     const int w0 = group_of(total, groups, f0), w1 = group_of(total, groups, f0 + run.units - 1);
     if (w0 == w1) return;
     const int n = w1 - w0 + 1, first = 2 * w0 + (f0 > first_unit(total, groups, w0) ? 1 : 0);
@@ -838,7 +872,7 @@ bool cache_ws(const CacheShape& s, CacheWs* w) {
     const int esz = s.dtype == PROXYATTN_BF16 ? 2 : 4;
     w->tiles = (int)std::min<int64_t>((rows + 15) / 16, esz == 2 ? 4 : 2);
     const int unit = 64 * key_tiles(s.fp4, esz, s.d);
-    const int64_t units = (s.max_len + unit - 1) / unit, flat = units + kStartUnits;
+    const int64_t units = (s.max_len + unit - 1) / unit, flat = units + start_units(s.fp4, w->tiles);
     const int64_t runs = (int64_t)s.b * s.hkv * max_row_tiles(s, w->tiles);
     // a workgroup of 256 threads to each run in the second launch
     if (rows > INT32_MAX || runs > INT32_MAX / 256 || runs * flat > INT32_MAX) return false;
@@ -877,7 +911,7 @@ static void attention_as(const CacheShape& s, const void* q, const int* table, c
     constexpr int UNIT = 64 * key_tiles(FP4, sizeof(T), D);
     const int rows = std::min(16 * NR, s.rep * s.max_new);
     const dim3 grid((unsigned)s.b * s.hkv * mt, rows);
-    cache_join_kernel<T, D, NR, UNIT><<<grid, 256, 0, st>>>(s, lens, starts, mt, w.groups, plan,
+    cache_join_kernel<T, D, NR, UNIT, start_units(FP4, NR)><<<grid, 256, 0, st>>>(s, lens, starts, mt, w.groups, plan,
                                                             stat, part, (T*)out, lse);
 }
 
