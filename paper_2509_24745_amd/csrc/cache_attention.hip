@@ -863,6 +863,20 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheShape s, const int
         lse[i * s.t + t] = sum > 0.f ? (hi + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
 }
 
+// 16-row tiles of a workgroup's rows.  As few row tiles of at most 64 rows as
+// there can be, equally full, where the keys' bytes bound the time.  4-bit keys cost more
+// to unpack than to read: past 48 rows, two workgroups of 32 rows on a CU beat one of
+// 64 (us, 12 sequences of up to 20K, d 128, most tiles 2, 3, 4: bf16 with 36 rows 122, 75,
+// 75; 64 rows 119, 125, 82; 96 rows 174, 129, 144; 4 bits 59, 53, 53; 61, 90, 69; 82, 93,
+// 118).  fp32 rows fill the registers with two.
+static int row_tiles(int64_t rows, bool fp4, int esz) {
+    const int64_t n = (rows + 15) / 16;
+    if (esz == 4) return (int)std::min<int64_t>(n, 2);
+    if (fp4) return n <= 3 ? (int)n : 2;
+    const int64_t parts = (n + 3) / 4;
+    return (int)((n + parts - 1) / parts);
+}
+
 static int max_row_tiles(const CacheShape& s, int tiles) {
     return (int)(((int64_t)s.rep * s.max_new + 16 * tiles - 1) / (16 * tiles));
 }
@@ -870,7 +884,7 @@ static int max_row_tiles(const CacheShape& s, int tiles) {
 bool cache_ws(const CacheShape& s, CacheWs* w) {
     const int64_t rows = (int64_t)s.rep * s.max_new;
     const int esz = s.dtype == PROXYATTN_BF16 ? 2 : 4;
-    w->tiles = (int)std::min<int64_t>((rows + 15) / 16, esz == 2 ? 4 : 2);
+    w->tiles = row_tiles(rows, s.fp4, esz);
     const int unit = 64 * key_tiles(s.fp4, esz, s.d);
     const int64_t units = (s.max_len + unit - 1) / unit, flat = units + start_units(s.fp4, w->tiles);
     const int64_t runs = (int64_t)s.b * s.hkv * max_row_tiles(s, w->tiles);
@@ -923,15 +937,23 @@ hipError_t launch_cache_attention(const CacheShape& s, const void* q, const int*
         typedef typename decltype(t)::type T;
         constexpr int D = decltype(d)::value;
         constexpr bool F = decltype(fp4)::value;
+        auto run = [&](auto nr) {
+            attention_as<T, D, F, decltype(nr)::value>(s, q, table, lens, starts, pg, out, lse, ws,
+                                                       w, st);
+        };
         if (w.tiles == 1)
-            attention_as<T, D, F, 1>(s, q, table, lens, starts, pg, out, lse, ws, w, st);
+            run(std::integral_constant<int, 1>());
         else if (w.tiles == 2)
-            attention_as<T, D, F, 2>(s, q, table, lens, starts, pg, out, lse, ws, w, st);
+            run(std::integral_constant<int, 2>());
         else if constexpr (sizeof(T) == 2) {
-            if (w.tiles == 3)
-                attention_as<T, D, F, 3>(s, q, table, lens, starts, pg, out, lse, ws, w, st);
-            else
-                attention_as<T, D, F, 4>(s, q, table, lens, starts, pg, out, lse, ws, w, st);
+            if constexpr (F) {
+                run(std::integral_constant<int, 3>());
+            } else {
+                if (w.tiles == 3)
+                    run(std::integral_constant<int, 3>());
+                else
+                    run(std::integral_constant<int, 4>());
+            }
         }
     });
     return hipGetLastError();
