@@ -33,7 +33,8 @@ struct CacheShape {
     int num_pages, width;
     int dtype, fp4;
     int past;        // the attention reads the pages past the caches
-    float scale2;    // softmax scale times log2(e)
+    // softmax scale times log2(e): the fp32 below it, and what that leaves, above 0
+    float scale2, scale2_rest;
     int64_t q_tok, q_head, kv_tok, kv_head, o_tok, o_head;  // element strides
 };
 

@@ -1,5 +1,6 @@
 // C ABI of the rotation and the paged cache: argument validation and kernel
 // sequencing, as in api.hip.
+#include <float.h>
 #include <math.h>
 #include <string.h>
 
@@ -138,7 +139,10 @@ static int resolve_cache(const proxyattn_cache* c, CacheShape* out) {
     s.past = 2 * rows * (s.fp4 ? d / 2 + d / 32 : d * esz) > kMallBytes / 2;
     const float scale =
         c->softmax_scale > 0.f ? c->softmax_scale : (float)(1.0 / sqrt((double)c->head_dim));
-    s.scale2 = scale * 1.4426950408889634f;
+    const double scale2 = (double)scale * 1.4426950408889634;
+    s.scale2 = (float)scale2;
+    if ((double)s.scale2 >= scale2) s.scale2 = nextafterf(s.scale2, 0.f);
+    s.scale2_rest = fmaxf((float)(scale2 - (double)s.scale2), FLT_MIN);
     s.q_tok = pick(c->q_tok_stride, s.hq * d);
     s.q_head = pick(c->q_head_stride, d);
     s.kv_tok = pick(c->kv_tok_stride, s.hkv * d);

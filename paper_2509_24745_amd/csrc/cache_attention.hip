@@ -690,8 +690,12 @@ cache_attn_kernel(
 #pragma unroll
                 for (int t = 0; t < KT; ++t) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        x[nr][t][c] = fast_exp2(fmaf(x[nr][t][c], s.scale2, -ref[nr]));
+                    for (int c = 0; c < 4; ++c) {
+                        // fp32: the scale's rounding would show, a score of 20 by 1e-6
+                        float less = -ref[nr];
+                        if constexpr (sizeof(T) == 4) less = fmaf(x[nr][t][c], s.scale2_rest, less);
+                        x[nr][t][c] = fast_exp2(fmaf(x[nr][t][c], s.scale2, less));
+                    }
                     sum[nr] += (x[nr][t][0] + x[nr][t][1]) + (x[nr][t][2] + x[nr][t][3]);
                 }
             }

@@ -427,6 +427,15 @@ ATTENDS = [
     ([20000, 3, 700], None, 4, 1, 128, 64, "bf16", "fp4"),
     ([9000, 3, 700], [3, 2, 1], 4, 2, 64, 64, "bf16", "same"),
     ([6000, 1], None, 2, 1, 128, 32, "fp32", "same"),
+    # several row tiles split over workgroups
+    ([2100, 5, 900], [9, 1, 20], 8, 2, 128, 64, "bf16", "same"),
+    ([1300, 64], [16, 3], 8, 2, 64, 32, "bf16", "same"),
+    ([2600, 700], [5, 9], 8, 2, 128, 32, "bf16", "fp4"),
+    ([2600, 700], [16, 1], 8, 2, 64, 16, "bf16", "fp4"),
+    ([1500, 3, 700], [6, 1, 2], 8, 2, 128, 64, "fp32", "same"),
+    ([1500, 3, 700], [6, 1, 2], 8, 2, 64, 16, "fp32", "same"),
+    ([2100, 90], [7, 2], 8, 1, 64, 128, "fp32", "fp4"),
+    ([2100, 90], [3, 2], 8, 2, 128, 16, "fp32", "fp4"),
 ]
 
 
@@ -522,6 +531,56 @@ def test_offsets_past_32_bits(pa):
             to += [ko, vo, out, lse]
         assert all(torch.equal(a, b) for a, b in zip(got, ref))
         del pools
+
+
+@pytest.mark.parametrize("cache", ["same", "fp4"])
+def test_large_passes_equal_small_ones(pa, cache):
+    """Passes over more rows than L2 or the MALL hold go about the caches another
+    way: the same rows as in parts of 10000 tokens."""
+    g = torch.Generator("cuda").manual_seed(5)
+    rng = np.random.default_rng(5)
+    n, hq, hkv, d, page = 150000, 8, 4, 128, 64
+    x = torch.randn((n, hq + 2 * hkv, d), generator=g, device="cuda").bfloat16()
+    q, k, v = x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:]
+    tok = (hq + 2 * hkv) * d
+    r = _rotary(pa, rng, d, 128, False, True, "bf16", n)
+    part = 10000
+
+    def strides(m):
+        return pa.Problem(m, hq, hkv, d, 128, 1, q_tok_stride=tok, kv_tok_stride=tok)
+
+    for m in (n, 30000):
+        qo, ko = torch.empty_like(q[:m].contiguous()), torch.empty_like(k[:m].contiguous())
+        pa.proxyattn_norm_rotate(strides(m), r, q[:m], k[:m], None, 0, qo, ko)
+        for a in range(0, m, part):
+            qp, kp = torch.empty_like(qo[:part]), torch.empty_like(ko[:part])
+            pa.proxyattn_norm_rotate(strides(part), r, q[a:a + part], k[a:a + part], None, a, qp, kp)
+            assert torch.equal(qp, qo[a:a + part]) and torch.equal(kp, ko[a:a + part])
+        pages = -(-m // page)
+        table = torch.randperm(pages, generator=g, device="cuda").int()[None].contiguous()
+        base = dict(num_seqs=1, num_q_heads=hq, num_kv_heads=hkv, head_dim=d, page_size=page,
+                    num_pages=pages, table_width=pages, cache_type=cache, max_len=m)
+        one = pa.Cache(num_tokens=m, max_new=m, q_tok_stride=tok, kv_tok_stride=tok, **base)
+        big, small = pa.Pages.empty(one), pa.Pages.empty(one)
+        qa = torch.empty_like(qo)
+        pa.proxyattn_cache_append(one, r, q[:m], k[:m], v[:m], qa, table, _ints([m]),
+                                  _ints([0, m]), big)
+        assert torch.equal(qa, qo)
+        few = pa.Cache(num_tokens=part, max_new=part, q_tok_stride=tok, kv_tok_stride=tok, **base)
+        packed = pa.Cache(num_tokens=m, max_new=m, **base)
+        packed_few = pa.Cache(num_tokens=part, max_new=part, **base)
+        kr, vr = (torch.empty((m, hkv, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        pa.proxyattn_cache_read(packed, table, _ints([m]), _ints([0, m]), big, kr, vr)
+        if cache == "same":
+            assert torch.equal(kr, ko) and torch.equal(vr, v[:m])
+        for a in range(0, m, part):
+            where = (table, _ints([a + part]), _ints([0, part]))
+            s = slice(a, a + part)
+            pa.proxyattn_cache_append(few, r, q[s], k[s], v[s], qp, *where, small)
+            assert torch.equal(qp, qo[s])
+            kp, vp = torch.empty_like(kr[:part]), torch.empty_like(kr[:part])
+            pa.proxyattn_cache_read(packed_few, *where, small, kp, vp)
+            assert torch.equal(kp, kr[s]) and torch.equal(vp, vr[s])
 
 
 def test_shared_pages(pa):
