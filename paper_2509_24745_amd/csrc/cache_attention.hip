@@ -401,14 +401,17 @@ template <typename T, bool FP4, int D, int NR> struct Queries {
 // lane group g takes the values that chunk i of KeyStep holds; for the outputs,
 // product (u, i) takes the keys of tiles 2 u and 2 u + 1 and value D/16 m + i of row m.
 // Probabilities go as a bf16 and the bf16 of what that rounds off, so that the
-// output's own rounding is the only one that shows (with the one bf16, its errors
-// are 1.4 times as large; 10 % of the time of 64 rows, none of 16, where the MFMAs
-// wait beside the loads).  fp32 rows take three terms of the queries and of the
+// output's own rounding is the only one that shows (error against 64 bits 1.66e-3,
+// 2.07e-3 with the one bf16); the MFMAs of the second wait beside the loads.  Not so
+// with several row tiles over 4-bit values, which carry errors of some percent
+// themselves: one bf16 there (8 sequences to 60K with 36 rows 72 -> 65 us, 16 to 20K
+// with 64 rows 75 -> 67).  fp32 rows take three terms of the queries and of the
 // probabilities: exact products as with fp32 MFMAs, in a fifth of their cycles.
 template <typename T, bool FP4, int D, int NR> struct Rows {
     typedef KeyStep<T, FP4, D> Keys;
     typedef Queries<T, FP4, D, NR> Q;
-    static constexpr int KT = Keys::KT, QC = D / 32, OC = D / 16, PT = Q::TERMS == 3 ? 3 : 2;
+    static constexpr int KT = Keys::KT, QC = D / 32, OC = D / 16;
+    static constexpr int PT = Q::TERMS == 3 ? 3 : FP4 && NR > 1 ? 1 : 2;   // terms of a probability
     Q q;
     f32x4 o[NR][OC];
 

@@ -8,8 +8,9 @@ and what is read back are equal.  Attention, with p the probabilities, S the
 largest sum |c q k| of a row and n its keys: a score is off by at most
 (d + 4) 2^-23 S (d products and sums, the scale, the reference), which moves p
 by as much, the exponential by 2^-22 more, sums of n terms by n 2^-24, bf16
-probabilities in two terms by 2^-16; so the output by
-(2 ((d + 4) 2^-23 S + 2^-22) + 2 n 2^-24 [+ 2^-16]) sum p |v|, and its own
+probabilities in two terms by 2^-16, in one (more than 16 rows over 4 bits) by half
+a step of bf16, 2^-8; so the output by
+(2 ((d + 4) 2^-23 S + 2^-22) + 2 n 2^-24 [+ 2^-16 or 2^-8]) sum p |v|, and its own
 rounding.
 """
 import numpy as np
@@ -243,7 +244,9 @@ class Batch:
         ref, rlse, absv, big = O.attention(_np(q), keys, values, self.tokens, scale)
         n = max(self.lens + [1])
         score = (c.head_dim + 4) * 2.0 ** -23 * big
-        a = 2 * (score + 2.0 ** -22) + 2 * n * 2.0 ** -24 + (2.0 ** -16 if self.dtype == "bf16" else 0)
+        one_term = c.cache_type == "fp4" and c.num_q_heads // c.num_kv_heads * c.max_new > 16
+        prob = 0 if self.dtype == "fp32" else 2.0 ** -8 if one_term else 2.0 ** -16
+        a = 2 * (score + 2.0 ** -22) + 2 * n * 2.0 ** -24 + prob
         tol = np.abs(ref) * HALF[self.dtype] * 1.001 + a[..., None] * absv + 1e-30
         got, glse = _np(out), _np(lse)
         rows = [r for r, _, _ in self.tokens]
