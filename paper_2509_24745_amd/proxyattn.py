@@ -206,6 +206,14 @@ class Problem:
     def torch_dtype(self):
         return torch.bfloat16 if self.dtype == "bf16" else torch.float32
 
+    @cached_property
+    def _rotated(self):
+        """What proxyattn_norm_rotate looks at: rows of q and of k, the struct."""
+        n, hq, hkv, d = self.seq_len, self.num_q_heads, self.num_kv_heads, self.head_dim
+        return (_Rows(n, hq, d, self.q_tok_stride, self.q_head_stride),
+                _Rows(n, hkv, d, self.kv_tok_stride, self.kv_head_stride),
+                ctypes.byref(self.c_struct()))
+
     def c_struct(self) -> proxyattn_problem:
         p = proxyattn_problem()
         p.struct_size = ctypes.sizeof(proxyattn_problem)
@@ -515,6 +523,26 @@ def _arg(x, n_elems: int, name: str, dtype, device: int, contiguous: bool = True
     return x.data_ptr()
 
 
+class _Rows:
+    """Token rows [n][heads][d] with strides (0: packed) as a call reads or writes them."""
+
+    __slots__ = ("shape", "stride", "span")
+
+    def __init__(self, n, heads, d, tok_stride, head_stride):
+        self.shape = (n, heads, d)
+        self.stride = (tok_stride or heads * d, head_stride or d, 1)
+        self.span = _span(n, heads, d, tok_stride, head_stride)
+
+    def arg(self, x, name: str, dtype, device: int) -> int | None:
+        """As _arg; a tensor of just this shape and these strides is looked at once."""
+        if x is None or type(x) is int:
+            return x
+        if not (x.dtype is dtype and x.shape == self.shape and x.stride() == self.stride
+                and x.get_device() == device >= 0):
+            _need(x, self.span, name, dtype, contiguous=False)
+        return x.data_ptr()
+
+
 _gpu_seen = False
 
 
@@ -571,6 +599,16 @@ class Rotary:
         r.k_out_tok_stride, r.k_out_head_stride = self.k_out_tok_stride, self.k_out_head_stride
         return r
 
+    def _out_rows(self, n: int, hq: int, hkv: int, d: int) -> tuple[_Rows, _Rows]:
+        """Rows of the outputs."""
+        held = self.__dict__.get("_rows")
+        if held is None or held[0] != (n, hq, hkv, d):
+            held = ((n, hq, hkv, d),
+                    (_Rows(n, hq, d, self.q_out_tok_stride, self.q_out_head_stride),
+                     _Rows(n, hkv, d, self.k_out_tok_stride, self.k_out_head_stride)))
+            self.__dict__["_rows"] = held
+        return held[1]
+
     def _arg(self, d: int, dtype, device: int):
         """The struct, by reference; its tensors checked once for a use (and
         again should they have moved)."""
@@ -598,17 +636,15 @@ def proxyattn_norm_rotate(prob: Problem, rotary: Rotary, q, k, positions, first_
     dev, st = _device_and_stream(stream)
     n, hq, hkv, d = prob.seq_len, prob.num_q_heads, prob.num_kv_heads, prob.head_dim
     dt = prob.torch_dtype
-    r = rotary._arg(d, dt, dev) if rotary is not None else None
-    nqo = nko = 0
+    qr, kr, p = prob._rotated
+    r = qo = ko = None
     if rotary is not None:
-        nqo = _span(n, hq, d, rotary.q_out_tok_stride, rotary.q_out_head_stride)
-        nko = _span(n, hkv, d, rotary.k_out_tok_stride, rotary.k_out_head_stride)
-    args = (_arg(q, _span(n, hq, d, prob.q_tok_stride, prob.q_head_stride), "q", dt, dev, False),
-            _arg(k, _span(n, hkv, d, prob.kv_tok_stride, prob.kv_head_stride), "k", dt, dev, False),
-            _arg(positions, n, "positions", torch.int32, dev), int(first_position),
-            _arg(q_out, nqo, "q_out", dt, dev, False), _arg(k_out, nko, "k_out", dt, dev, False))
-    p = prob.c_struct()
-    _check(lib().proxyattn_norm_rotate(ctypes.byref(p), r, *args, st))
+        r = rotary._arg(d, dt, dev)
+        qor, kor = rotary._out_rows(n, hq, hkv, d)
+        qo, ko = qor.arg(q_out, "q_out", dt, dev), kor.arg(k_out, "k_out", dt, dev)
+    _check(lib().proxyattn_norm_rotate(p, r, qr.arg(q, "q", dt, dev), kr.arg(k, "k", dt, dev),
+                                       _arg(positions, n, "positions", torch.int32, dev),
+                                       int(first_position), qo, ko, st))
 
 
 @dataclass(frozen=True)
@@ -662,13 +698,13 @@ class Cache:
 
     @cached_property
     def _sizes(self):
-        """Elements that a call touches: q, kv, out spans; a page pool; its scales."""
+        """Rows of q, of k and v and of out; elements of a page pool and of its scales."""
         t, hq, hkv, d = self.num_tokens, self.num_q_heads, self.num_kv_heads, self.head_dim
         rows = self.num_pages * hkv * self.page_size
         fp4 = self.cache_type == "fp4"
-        return (_span(t, hq, d, self.q_tok_stride, self.q_head_stride),
-                _span(t, hkv, d, self.kv_tok_stride, self.kv_head_stride),
-                _span(t, hq, d, self.o_tok_stride, self.o_head_stride),
+        return (_Rows(t, hq, d, self.q_tok_stride, self.q_head_stride),
+                _Rows(t, hkv, d, self.kv_tok_stride, self.kv_head_stride),
+                _Rows(t, hq, d, self.o_tok_stride, self.o_head_stride),
                 rows * (d // 2 if fp4 else d), rows * (d // 32) if fp4 else 0)
 
     @cached_property
@@ -747,12 +783,16 @@ def proxyattn_cache_append(cache: Cache, rotary: Rotary | None, q, k, v, q_out, 
                            seq_lens, new_start, pages: Pages, stream=None):
     dev, st = _device_and_stream(stream)
     dt = cache.torch_dtype
-    nq, nkv = cache._sizes[:2]
-    r = rotary._arg(cache.head_dim, dt, dev) if rotary is not None else None
-    out = _span(cache.num_tokens, cache.num_q_heads, cache.head_dim, rotary.q_out_tok_stride,
-                rotary.q_out_head_stride) if rotary is not None else 0
-    args = (_arg(q, nq, "q", dt, dev, False), _arg(k, nkv, "k", dt, dev, False),
-            _arg(v, nkv, "v", dt, dev, False), _arg(q_out, out, "q_out", dt, dev, False))
+    qr, kvr, _, _, _ = cache._sizes
+    r = None
+    if rotary is not None:
+        r = rotary._arg(cache.head_dim, dt, dev)
+        rows = rotary._out_rows(cache.num_tokens, cache.num_q_heads, cache.num_kv_heads,
+                                cache.head_dim)[0]
+        qo = rows.arg(q_out, "q_out", dt, dev)
+    else:
+        qo = _ptr(q_out)   # refused by the library
+    args = (qr.arg(q, "q", dt, dev), kvr.arg(k, "k", dt, dev), kvr.arg(v, "v", dt, dev), qo)
     batch = _arg_batch(cache, page_table, seq_lens, new_start, pages, dev)
     _check(lib().proxyattn_cache_append(cache._ref, r, *args, *batch, st))
 
@@ -760,9 +800,8 @@ def proxyattn_cache_append(cache: Cache, rotary: Rotary | None, q, k, v, q_out, 
 def proxyattn_cache_read(cache: Cache, page_table, seq_lens, new_start, pages: Pages, k_out,
                          v_out, stream=None):
     dev, st = _device_and_stream(stream)
-    nkv = cache._sizes[1]
-    outs = (_arg(k_out, nkv, "k_out", cache.torch_dtype, dev, False),
-            _arg(v_out, nkv, "v_out", cache.torch_dtype, dev, False))
+    dt, kvr = cache.torch_dtype, cache._sizes[1]
+    outs = (kvr.arg(k_out, "k_out", dt, dev), kvr.arg(v_out, "v_out", dt, dev))
     batch = _arg_batch(cache, page_table, seq_lens, new_start, pages, dev)
     _check(lib().proxyattn_cache_read(cache._ref, *batch, *outs, st))
 
@@ -771,10 +810,10 @@ def proxyattn_cache_attention(cache: Cache, q, page_table, seq_lens, new_start, 
                               lse, workspace, stream=None):
     dev, st = _device_and_stream(stream)
     dt = cache.torch_dtype
-    nq, _, no, _, _ = cache._sizes
-    qp = _arg(q, nq, "q", dt, dev, False)
+    qr, _, outr, _, _ = cache._sizes
+    qp = qr.arg(q, "q", dt, dev)
     batch = _arg_batch(cache, page_table, seq_lens, new_start, pages, dev)
-    op = _arg(out, no, "out", dt, dev, False)
+    op = outr.arg(out, "out", dt, dev)
     lp = _arg(lse, cache.num_q_heads * cache.num_tokens, "lse", torch.float32, dev)
     need = ws_bytes = cache._workspace_bytes
     if isinstance(workspace, torch.Tensor):
