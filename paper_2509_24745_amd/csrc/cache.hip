@@ -64,7 +64,7 @@ template <> struct Chunk<bf16> {
     __device__ __forceinline__ float at(int e) const { return get_elem<bf16>(w, e); }
     __device__ __forceinline__ void from(const float (&x)[8]) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
+        for (int j = 0; j < 4; ++j) w[j] = pack_rne(x[2 * j], x[2 * j + 1]);
     }
 };
 template <> struct Chunk<float> {

@@ -24,6 +24,15 @@ __device__ __forceinline__ int seq_of_token(const int* starts, int b, int t) {
     return base + __popcll(__ballot(lane < step && starts[min(base + lane + 1, b)] <= t));
 }
 
+// Two values rounded to bf16 (nearest, ties to even), the first low, by the
+// hardware's conversion.
+__device__ __forceinline__ uint32_t pack_rne(float lo, float hi) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const f32x2 x = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+}
+
 // The eight 4-bit values of a word.
 __device__ __forceinline__ void fp4_values(uint32_t w, float scale, float (&z)[8]) {
     const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0);
