@@ -406,13 +406,17 @@ template <typename T, bool FP4, int D, int NR> struct Rows {
     typedef Queries<T, FP4, D, NR> Q;
     static constexpr int KT = Keys::KT, QC = D / 32, OC = D / 16;
     static constexpr int PT = Q::TERMS == 3 ? 3 : FP4 && NR > 1 ? 1 : 2;   // terms of a probability
+    // With two and four row tiles the scheduler would spread a step's conversions
+    // until registers spill (16 sequences to 20K in 4 bits, 64 rows: 96 instead of 67 us);
+    // three fit, and gain 3-6 % from the overlap.
+    static constexpr bool kApart = NR == 2 || NR == 4;
     Q q;
     f32x4 o[NR][OC];
 
     __device__ __forceinline__ void scores(const Keys& ks, int lane, f32x4 (&x)[NR][KT]) const {
 #pragma unroll
         for (int t0 = 0; t0 < KT; t0 += 2) {
-            if constexpr (NR > 1) __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kApart) __builtin_amdgcn_sched_barrier(0);
             bf16x8 kf[2][QC];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -447,7 +451,7 @@ template <typename T, bool FP4, int D, int NR> struct Rows {
     __device__ __forceinline__ void outputs(const Keys& ks, const f32x4 (&p)[NR][KT]) {
 #pragma unroll
         for (int u = 0; u < KT / 2; ++u) {
-            if constexpr (NR > 1) __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kApart) __builtin_amdgcn_sched_barrier(0);
             bf16x8 pf[NR][PT];
 #pragma unroll
             for (int nr = 0; nr < NR; ++nr) {
@@ -463,7 +467,6 @@ template <typename T, bool FP4, int D, int NR> struct Rows {
 #pragma unroll
                 for (int k = 0; k < PT; ++k) pf[nr][k] = as_frag(f[k]);
             }
-            if constexpr (NR > 2) __builtin_amdgcn_sched_barrier(0);
             // slots 2 w, 2 w + 1 of the fragment: keys KT r + 2 u + w / 2, r = 2 (w % 2) and the next
 #pragma unroll
             for (int c = 0; c < OC / 2; ++c) {   // values 2 c and 2 c + 1 of the lane's
@@ -571,7 +574,9 @@ cache_attn_kernel(
     constexpr int KT = Keys::KT, SK = 16 * KT, UNIT = 4 * SK, ROWS = 16 * NR, OC = D / 16;
     constexpr int START = start_units(FP4, NR);
     constexpr int LINE = D + 4;   // a row's outputs in LDS, padded by a bank group
-    __shared__ __align__(16) float merge[4][16][LINE];
+    // all row tiles at once where their outputs and another workgroup fit into LDS
+    constexpr int MT = sizeof(T) == 2 ? NR : 1;
+    __shared__ __align__(16) float merge[4][16 * MT][LINE];
     __shared__ float2 wstat[4][ROWS];
     __shared__ __align__(16) typename Queries<T, FP4, D, NR>::E queries[Queries<T, FP4, D, NR>::LDS];
     const int lane = threadIdx.x & 63, wave = wave_uniform(threadIdx.x >> 6);
@@ -727,46 +732,48 @@ cache_attn_kernel(
             }
         }
 
-        // the four waves' rows together
+        // the four waves' rows together, MT row tiles at a time
         const bool whole = u0 == 0 && u1 == run.units;
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr) {
             sum[nr] = groups_sum(sum[nr]);
             if (g == 0) wstat[wave][16 * nr + n] = float2{ref[nr], sum[nr]};
         }
-        __syncthreads();
 #pragma unroll
-        for (int nr = 0; nr < NR; ++nr) {
-            float top = kNoScore;
+        for (int m0 = 0; m0 < NR; m0 += MT) {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) top = fmaxf(top, wstat[w][16 * nr + n].x);
-            const float shrink = fast_exp2(ref[nr] - top);
+            for (int nr = m0; nr < m0 + MT; ++nr)
 #pragma unroll
-            for (int c = 0; c < 4; ++c)   // values OC (4 g + c) ..
+                for (int c = 0; c < 4; ++c)   // values OC (4 g + c) ..
 #pragma unroll
-                for (int i = 0; i < OC; i += 4)
-                    *reinterpret_cast<f32x4*>(&merge[wave][n][OC * (4 * g + c) + i]) =
-                        f32x4{r.o[nr][i][c], r.o[nr][i + 1][c], r.o[nr][i + 2][c],
-                              r.o[nr][i + 3][c]} * shrink;
+                    for (int i = 0; i < OC; i += 4)
+                        *reinterpret_cast<f32x4*>(
+                            &merge[wave][16 * (nr - m0) + n][OC * (4 * g + c) + i]) =
+                            f32x4{r.o[nr][i][c], r.o[nr][i + 1][c], r.o[nr][i + 2][c],
+                                  r.o[nr][i + 3][c]};
             __syncthreads();
-            // 16 rows of D/8 pieces of 8 values
+            // rows of D/8 pieces of 8 values
             const int piece = threadIdx.x % (D / 8);
-            for (int line = threadIdx.x / (D / 8); line < 16; line += kAttnThreads / (D / 8)) {
-                const int row = row0 + 16 * nr + line;
+            for (int line = threadIdx.x / (D / 8); line < 16 * MT;
+                 line += kAttnThreads / (D / 8)) {
+                const int at = 16 * m0 + line, row = row0 + at;
                 if (row >= rows) break;
-                float z[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) z[j] = 0.f;
-                float hi = kNoScore, l = 0.f;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) hi = fmaxf(hi, wstat[w][16 * nr + line].x);
+                float2 st[4];
+                float hi = kNoScore, l = 0.f, z[8];
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const float2 st = wstat[w][16 * nr + line];
-                    l += st.y * fast_exp2(st.x - hi);
+                    st[w] = wstat[w][at];
+                    hi = fmaxf(hi, st[w].x);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z[j] = 0.f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const float k = fast_exp2(st[w].x - hi);
+                    l += st[w].y * k;
                     const float* m = &merge[w][line][8 * piece];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) z[j] += m[j];
+                    for (int j = 0; j < 8; ++j) z[j] += m[j] * k;
                 }
                 if (whole) {
                     const int j = token_of(row);
@@ -778,8 +785,8 @@ cache_attn_kernel(
                     if (lse && piece == 0)
                         lse[i * s.t + t] = l > 0.f ? (hi + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
                 } else {
-                    store8<float>(part + ((int64_t)slot * ROWS + 16 * nr + line) * D + 8 * piece, z);
-                    if (piece == 0) stat[(int64_t)slot * ROWS + 16 * nr + line] = float2{hi, l};
+                    store8<float>(part + ((int64_t)slot * ROWS + at) * D + 8 * piece, z);
+                    if (piece == 0) stat[(int64_t)slot * ROWS + at] = float2{hi, l};
                 }
             }
             __syncthreads();
