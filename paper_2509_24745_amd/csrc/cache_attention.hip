@@ -795,80 +795,110 @@ cache_attn_kernel(
 }
 
 // Rows cut between workgroups: their partial rows added up in the order of
-// the keys.  A workgroup to a row: run (sequence, head, tile) blockIdx.x, row
-// blockIdx.y of it.  D/4 threads hold a partial row, 256 / (D/4) partial rows
-// are read side by side, the first four of each before anything is known of
-// their references.
-template <typename T, int D, int NR, int UNIT, int START>
+// the keys.  TEAM threads (a workgroup or a wave) to a row, the workgroup's rows all of
+// one run (sequence, head, tile) blockIdx.x.  D/4 threads hold a partial row, the
+// team reads TEAM / (D/4) partial rows side by side, the first EARLY of each thread
+// before anything is known of their references.  Whole workgroups are for few rows
+// of many parts (8 runs of 4 rows in 64 parts: 4.1 us), waves for many rows, of which
+// most were not cut (128 runs of 64 rows: 14.1 -> 6.6 us).
+template <typename T, int D, int NR, int UNIT, int START, int TEAM>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheShape s, const int* lens,
                                                          const int* starts, int max_tiles,
                                                          int groups, const int* plan,
                                                          const float2* stat, const float* part,
                                                          T* out, float* lse) {
-    constexpr int ROWS = 16 * NR, L4 = D / 4, SIDE = 256 / L4, EARLY = 4;
-    __shared__ float2 piece[kCacheGroups];
+    constexpr int ROWS = 16 * NR, L4 = D / 4, SIDE = TEAM / L4, EARLY = 4;
+    constexpr bool WAVE = TEAM == 64;
+    __shared__ float2 piece[WAVE ? 1 : kCacheGroups];
     __shared__ float top[4];
-    __shared__ __align__(16) float side[SIDE][D];
-    __shared__ float side_sum[SIDE];
-    const int tid = threadIdx.x, e = tid % L4, k = tid / L4, line = blockIdx.y;
+    __shared__ __align__(16) float side[WAVE ? 1 : SIDE][D];
+    __shared__ float side_sum[WAVE ? 1 : SIDE];
+    const int tid = threadIdx.x % TEAM, e = tid % L4, k = tid / L4;
+    const int line = blockIdx.y * (256 / TEAM) + threadIdx.x / TEAM;
     const int per_seq = s.hkv * max_tiles;
     const int b = blockIdx.x / per_seq, item = blockIdx.x - b * per_seq;
-    const int head = item / max_tiles, tile = item - head * max_tiles;
+    const int head = max_tiles == 1 ? item : item / max_tiles, tile = item - head * max_tiles;
     const Seq sq = seq_at(s, lens, starts, b);
     const int total = plan[s.b], base = plan[b];
     const Runs<ROWS, UNIT, START> run(s, sq);
     const int row = tile * ROWS + line;
-    if (tile >= run.tiles || row >= sq.fresh * s.rep) return;
+    if (tile >= run.tiles || line >= ROWS || row >= sq.fresh * s.rep) return;
     const int f0 = base + (head * run.tiles + tile) * run.flat() + START;
     const int w0 = group_of(total, groups, f0), w1 = group_of(total, groups, f0 + run.units - 1);
     if (w0 == w1) return;
     const int n = w1 - w0 + 1, first = 2 * w0 + (f0 > first_unit(total, groups, w0) ? 1 : 0);
     auto slot = [&](int i) { return (int64_t)(i ? 2 * (w0 + i) : first) * ROWS + line; };
+    auto values = [&](int i) {
+        return *reinterpret_cast<const f32x4*>(part + slot(i) * D + 4 * e);
+    };
     f32x4 early[EARLY];
 #pragma unroll
-    for (int i = 0; i < EARLY; ++i)
-        early[i] = *reinterpret_cast<const f32x4*>(part + slot(min(k + i * SIDE, n - 1)) * D + 4 * e);
+    for (int i = 0; i < EARLY; ++i) early[i] = values(min(k + i * SIDE, n - 1));
     float hi = kNoScore;
-    for (int i = tid; i < n; i += 256) {
-        piece[i] = stat[slot(i)];
-        hi = fmaxf(hi, piece[i].x);
+    for (int i = tid; i < n; i += TEAM) {
+        const float2 st = stat[slot(i)];
+        if constexpr (!WAVE) piece[i] = st;
+        hi = fmaxf(hi, st.x);
     }
     hi = wave_max(hi);
-    if ((tid & 63) == 0) top[tid >> 6] = hi;
-    __syncthreads();
-    hi = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    if constexpr (!WAVE) {
+        if ((tid & 63) == 0) top[tid >> 6] = hi;
+        __syncthreads();
+        hi = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    }
+    auto stat_of = [&](int i) { return WAVE ? stat[slot(i)] : piece[i]; };
     float l = 0.f;
     f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < EARLY; ++i)
         if (k + i * SIDE < n) {
-            const float2 st = piece[k + i * SIDE];
+            const float2 st = stat_of(k + i * SIDE);
             const float x = fast_exp2(st.x - hi);
             l += st.y * x;
             z += early[i] * x;
         }
 #pragma unroll 4
     for (int i = k + EARLY * SIDE; i < n; i += SIDE) {
-        const float2 st = piece[i];
+        const float2 st = stat_of(i);
         const float x = fast_exp2(st.x - hi);
         l += st.y * x;
-        z += *reinterpret_cast<const f32x4*>(part + slot(i) * D + 4 * e) * x;
+        z += values(i) * x;
     }
-    *reinterpret_cast<f32x4*>(&side[k][4 * e]) = z;
-    if (e == 0) side_sum[k] = l;
-    __syncthreads();
-    if (tid >= D) return;
-    float sum = 0.f, o = 0.f;
-#pragma unroll
-    for (int i = 0; i < SIDE; ++i) {
-        sum += side_sum[i];
-        o += side[i][tid];
-    }
-    const int j = row / s.rep;
+    const int j = sq.fresh == 1 ? 0 : row / s.rep;
     const int64_t t = sq.row + j, i = head * s.rep + row - j * s.rep;
-    out[t * s.o_tok + i * s.o_head + tid] = from_f32_rne<T>(sum > 0.f ? o / sum : 0.f);
+    T* const o = out + t * s.o_tok + i * s.o_head;
+    if constexpr (WAVE) {
+#pragma unroll
+        for (int x = L4; x < 64; x *= 2) {
+            l += __shfl_xor(l, x);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) z[c] += __shfl_xor(z[c], x);
+        }
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        if (k == 0) {
+            if constexpr (sizeof(T) == 2) {
+                u32x2 w = {pack_rne(z[0] * inv, z[1] * inv), pack_rne(z[2] * inv, z[3] * inv)};
+                *reinterpret_cast<u32x2*>(o + 4 * e) = w;
+            } else {
+                *reinterpret_cast<f32x4*>(o + 4 * e) = z * inv;
+            }
+        }
+    } else {
+        *reinterpret_cast<f32x4*>(&side[k][4 * e]) = z;
+        if (e == 0) side_sum[k] = l;
+        __syncthreads();
+        if (tid >= D) return;
+        float v = 0.f;
+        l = 0.f;
+#pragma unroll
+        for (int x = 0; x < SIDE; ++x) {
+            l += side_sum[x];
+            v += side[x][tid];
+        }
+        o[tid] = from_f32_rne<T>(l > 0.f ? v / l : 0.f);
+    }
     if (lse && tid == 0)
-        lse[i * s.t + t] = sum > 0.f ? (hi + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
+        lse[i * s.t + t] = l > 0.f ? (hi + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
 }
 
 // 16-row tiles of a workgroup's rows.  As few row tiles of at most 64 rows as
@@ -915,6 +945,10 @@ bool cache_ws(const CacheShape& s, CacheWs* w) {
     return true;
 }
 
+// Rows past which a wave, not a workgroup, adds a row's parts up: more would not be
+// on the GPU at once.
+constexpr int kJoinWaves = 2048;
+
 template <typename T, int D, bool FP4, int NR>
 static void attention_as(const CacheShape& s, const void* q, const int* table, const int* lens,
                          const int* starts, const PagePtrs& pg, void* out, float* lse, char* ws,
@@ -932,9 +966,15 @@ static void attention_as(const CacheShape& s, const void* q, const int* table, c
     if (!w.joined) return;
     constexpr int UNIT = 64 * key_tiles(FP4, sizeof(T), D);
     const int rows = std::min(16 * NR, s.rep * s.max_new);
-    const dim3 grid((unsigned)s.b * s.hkv * mt, rows);
-    cache_join_kernel<T, D, NR, UNIT, start_units(FP4, NR)><<<grid, 256, 0, st>>>(s, lens, starts, mt, w.groups, plan,
-                                                            stat, part, (T*)out, lse);
+    const unsigned runs = (unsigned)s.b * s.hkv * mt;
+    if ((int64_t)runs * rows > kJoinWaves)
+        cache_join_kernel<T, D, NR, UNIT, start_units(FP4, NR), 64>
+            <<<dim3(runs, (rows + 3) / 4), 256, 0, st>>>(s, lens, starts, mt, w.groups, plan, stat,
+                                                         part, (T*)out, lse);
+    else
+        cache_join_kernel<T, D, NR, UNIT, start_units(FP4, NR), 256>
+            <<<dim3(runs, rows), 256, 0, st>>>(s, lens, starts, mt, w.groups, plan, stat, part,
+                                               (T*)out, lse);
 }
 
 hipError_t launch_cache_attention(const CacheShape& s, const void* q, const int* table,
