@@ -434,16 +434,18 @@ int proxyattn_norm_rotate(const proxyattn_problem* p, const proxyattn_rotary* r,
  * All three: device, 4-byte aligned.  The library sees them only inside
  * kernels, so bad values cannot be refused; they never make a kernel leave
  * its arrays: lengths count up to max_len, new tokens of a sequence up to
- * max_new, a row at a position below 0 is a token of no sequence; a page outside
- * [0, num_pages) takes no token when appending, gives none when reading back and is
- * clamped in the attention.
+ * max_new; rows at positions below 0 are skipped when appending and reading back, and
+ * see nothing in the attention (out 0, lse -inf); a page outside [0, num_pages) takes no
+ * token when appending, gives none when reading back and is clamped in the
+ * attention.
  *
  * Two sequences may share pages (a common beginning) as long as no call
- * appends to a shared one; tokens appended to one slot by one call, which only
- * such a table gives, leave either.
+ * appends to a shared one: of tokens that one call appends to one slot, which only
+ * such a table gives, the slot holds parts of either.
  *
  * Supported: d in {64, 128}; page_size in {16, 32, 64, 128, 256}; B <= 4096;
- * Hq <= 4096, Hq % Hkv == 0; max_len <= table_width * page_size <= 2^30.
+ * num_tokens <= 2^26; Hq <= 4096, Hq % Hkv == 0; max_len <= table_width * page_size
+ * <= 2^30.
  */
 typedef struct proxyattn_cache {
     uint32_t struct_size;   /* = sizeof(proxyattn_cache) */
@@ -459,7 +461,7 @@ typedef struct proxyattn_cache {
     int32_t table_width;    /* row length of page_table */
     int32_t dtype;          /* of q, k, v and out: PROXYATTN_BF16 or PROXYATTN_F32 */
     int32_t cache_type;     /* PROXYATTN_CACHE_SAME or PROXYATTN_CACHE_FP4 */
-    float softmax_scale;    /* <= 0 selects 1/sqrt(d) */
+    float softmax_scale;    /* <= 0 selects 1/sqrt(d); else at least 2^-126 */
     /* token arrays [num_tokens][H][d]: strides in elements, 0 = packed */
     int64_t q_tok_stride, q_head_stride;
     int64_t kv_tok_stride, kv_head_stride; /* shared by K and V */

@@ -89,6 +89,8 @@ static int resolve_cache(const proxyattn_cache* c, CacheShape* out) {
                     c->num_tokens);
     if (c->num_seqs > kMaxSeqs)
         return fail(PROXYATTN_E_UNSUPPORTED, "num_seqs %d > %d", c->num_seqs, kMaxSeqs);
+    if (c->num_tokens > 1 << 26)   // workgroups of 256 threads to four tokens each
+        return fail(PROXYATTN_E_UNSUPPORTED, "num_tokens %d > 2^26", c->num_tokens);
     if (c->max_new < 1 || c->max_len < 1 || c->num_pages < 1 || c->table_width < 1)
         return fail(PROXYATTN_E_INVALID,
                     "max_new, max_len, num_pages and table_width must be positive");
@@ -115,6 +117,8 @@ static int resolve_cache(const proxyattn_cache* c, CacheShape* out) {
         return fail(PROXYATTN_E_UNSUPPORTED, "cache_type %d", c->cache_type);
     if (!finite((double)c->softmax_scale))
         return fail(PROXYATTN_E_INVALID, "softmax_scale is not finite");
+    if (c->softmax_scale > 0.f && c->softmax_scale < FLT_MIN)
+        return fail(PROXYATTN_E_INVALID, "softmax_scale below 2^-126");
     const int esz = c->dtype == PROXYATTN_BF16 ? 2 : 4;
     const int64_t d = c->head_dim;
     CacheShape s{};

@@ -472,6 +472,76 @@ def test_attention_of_many_sequences(pa, cache):
     w.check(q, *w.attend(q), keys, values)
 
 
+def test_most_sequences(pa):
+    """4096 sequences, most with a token, two long ones: the runs are dealt over
+    sequences that nobody keeps at hand."""
+    rng = np.random.default_rng(10)
+    lens = rng.integers(0, 4, 4096)
+    lens[[17, 4000]] = 2500
+    new = np.minimum(lens, 1)
+    w = Batch(pa, rng, lens.tolist(), new.tolist(), 2, 1, 64, 16, "bf16", "fp4")
+    keys, values = w.fill(rng)
+    q = _rand(rng, (w.cache.num_tokens, 2, 64), "bf16")
+    w.check(q, *w.attend(q), keys, values)
+
+
+def test_two_calls_at_once(pa):
+    """The same step of two batches on two streams, with a workspace each."""
+    rng = np.random.default_rng(11)
+    both = []
+    for i in range(2):
+        w = Batch(pa, rng, [3000, 40 + i, 900], [1, 1, 1], 8, 2, 128, 64, "bf16",
+                  "same" if i else "fp4", null_start=True)
+        keys, values = w.fill(rng)
+        q = _rand(rng, (3, 8, 128), "bf16")
+        both.append((w, keys, values, q, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for w, _, _, q, st in both:
+            with torch.cuda.stream(st):
+                got.append(w.attend(q))
+    torch.cuda.synchronize()
+    for i, (w, keys, values, q, _) in enumerate(both):
+        w.check(q, *got[i], keys, values)
+        for out, lse in got[i::2]:
+            assert torch.equal(out, got[i][0]) and torch.equal(lse, got[i][1])
+
+
+def test_append_queries_in_place(pa):
+    """Queries rotated where they lie, keys alone rotated (no queries), one side of
+    norm_rotate: all give what the separate arrays give."""
+    rng = np.random.default_rng(12)
+    hq, hkv, d, t = 6, 2, 64, 37
+    tok = (hq + 2 * hkv) * d
+    x = _rand(rng, (t, hq + 2 * hkv, d), "bf16")
+    q, k, v = x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:]
+    w = Batch(pa, rng, [50], [t], hq, hkv, d, 16, "bf16", "same", q_tok_stride=tok,
+              kv_tok_stride=tok)
+    r = _rotary(pa, rng, d, 32, True, True, "bf16", 50)
+    qo = torch.empty((t, hq, d), dtype=torch.bfloat16, device="cuda")
+    pa.proxyattn_cache_append(w.cache, r, q, k, v, qo, *w.where, w.pages)
+    first = (w.pages.k.clone(), w.pages.v.clone())
+    ko = torch.empty((t, hkv, d), dtype=torch.bfloat16, device="cuda")
+    prob = pa.Problem(t, hq, hkv, d, 64, 1, q_tok_stride=tok, kv_tok_stride=tok)
+    pa.proxyattn_norm_rotate(prob, r, None, k, None, 13, None, ko)
+    for p in (w.pages.k, w.pages.v):
+        p.fill_(float("nan"))
+    pa.proxyattn_cache_append(w.cache, r, None, k, v, None, *w.where, w.pages)
+    same = [torch.equal(a.view(torch.int16), b.view(torch.int16))
+            for a, b in zip(first, (w.pages.k, w.pages.v))]
+    assert all(same)
+    kr, vr = torch.empty_like(ko), torch.empty_like(ko)
+    pa.proxyattn_cache_read(pa.Cache(**{f: getattr(w.cache, f) for f in
+                                        w.cache.__dataclass_fields__ if "stride" not in f}),
+                            *w.where, w.pages, kr, vr)
+    assert torch.equal(kr, ko) and torch.equal(vr, v)
+    fields = ("rotary_dim", "interleaved", "eps", "cos", "sin", "q_weight", "k_weight")
+    here = pa.Rotary(**{f: getattr(r, f) for f in fields}, q_out_tok_stride=tok)
+    pa.proxyattn_cache_append(w.cache, here, q, k, v, q, *w.where, w.pages)
+    assert torch.equal(q, qo)
+
+
 def test_attention_scale_and_output_strides(pa):
     rng = np.random.default_rng(9)
     hq, d, t = 6, 128, 2
@@ -600,12 +670,14 @@ def test_shared_pages(pa):
     w.check(q, *w.attend(q), keys, values)
 
 
-def test_step_captured_and_replayed(pa):
+@pytest.mark.parametrize("long", [700, 3000])
+def test_step_captured_and_replayed(pa, long):
     """A decode step in a HIP graph, replayed while the lengths grow, each replay
-    against the eager step; two captured steps share a workspace."""
+    against the eager step; two captured steps share a workspace.  Runs of a
+    workgroup each (the shorter length) and runs that are cut."""
     rng = np.random.default_rng(15)
     hq, hkv, d = 8, 2, 128
-    w = Batch(pa, rng, [700, 64, 129], [1, 1, 1], hq, hkv, d, 64, "bf16", "fp4", null_start=True,
+    w = Batch(pa, rng, [long, 64, 129], [1, 1, 1], hq, hkv, d, 64, "bf16", "fp4", null_start=True,
               extra_width=2, spare_pages=12)
     w.fill(rng)
     free = sorted(set(range(w.cache.num_pages)) - set(w.table[w.table >= 0].tolist()))
@@ -613,9 +685,10 @@ def test_step_captured_and_replayed(pa):
         used = -(-w.lens[b] // 64)
         w.table[b, used] = free.pop()
     c = pa.Cache(**{**{f: getattr(w.cache, f) for f in w.cache.__dataclass_fields__},
-                    "max_len": 764})
+                    "max_len": long + 64})
+    assert (pa.proxyattn_cache_workspace_size(c) > 0) == (long == 3000)
     table = _ints(w.table.tolist())
-    r = _rotary(pa, rng, d, 128, False, True, "bf16", 800)
+    r = _rotary(pa, rng, d, 128, False, True, "bf16", long + 64)
     bufs = pa.CacheBuffers(c)
     eager = pa.CacheBuffers(c)
     bufs2 = pa.CacheBuffers(c)
