@@ -13,10 +13,10 @@
 // product, V as the 4 KT keys of the lane's group, D/16 values of each, and both go from
 // memory to registers: no other wave wants them.  What the MFMAs take for a
 // key's index or a value's is free as long as both operands agree, which is
-// what picks the orders here (see Compute).
+// what picks the orders here (see Rows).
 //
 // Work is dealt flat: every (sequence, KV head, row tile) is a run of units of
-// 64 KT keys, all runs lie end to end, and workgroup w of W takes the w-th
+// 64 KT keys (four waves' steps), all runs lie end to end, and workgroup w of W takes the w-th
 // equal part, whatever the lengths are.  A run cut between workgroups leaves
 // partial rows (reference, sum, output) in the workspace, added up in order by
 // a second launch.
@@ -45,9 +45,13 @@ constexpr float kSlack = 8.f;
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// 16-key tiles of a step: 64 keys in 4 bits, 32 in bf16 and in fp32 up to 64
-// values, 16 otherwise, so that two steps' keys and values fit beside the rows.
-constexpr int key_tiles(bool fp4, int esz, int d) { return fp4 ? 4 : esz * d > 256 ? 1 : 2; }
+// 16-key tiles of a step: 32 keys in 4 bits with one row tile, 64 with several,
+// 32 in bf16 and in fp32 up to 64 values, 16 otherwise, so that two steps' keys and
+// values fit beside the rows.  (4 bits, 64 and 32 keys, us: 64 sequences to 32K 34.9,
+// 33.6, one of 128K 36.9, 36.5; 8 to 60K with 36 rows 61, 75.)
+constexpr int key_tiles(bool fp4, int esz, int d, int nr) {
+    return fp4 ? (nr == 1 ? 2 : 4) : esz * d > 256 ? 1 : 2;
+}
 
 // Workgroups that a CU holds: as many as the registers allow.
 constexpr int groups_per_cu(bool fp4, int esz, int d, int nr) {
@@ -64,9 +68,9 @@ constexpr int start_units(bool fp4, int nr) { return fp4 ? 2 : nr == 1 ? 1 : 3; 
 // Up to so many units a run is a workgroup's own, by the number of runs: one
 // launch, and nobody looks up who has what.  Calls in a graph, 32 query heads on 8,
 // d 128, whole against cut (us): 1 sequence (8 runs) of 512 keys in bf16 (4 units)
-// 8.6 / 9.2, of 1024 13.0 / 9.3; 8 sequences of 1024 13.9 / 16.2, 4 bits 2048 (8
-// units) 15.2 / 14.6; 64 of 1024 44.7 / 49.5.  Longer runs of many sequences gain
-// as much where their lengths are equal, but lose more where they are not.
+// 8.5 / 8.8, of 1024 12.7 / 8.7; 8 sequences of 1024 13.6 / 15.7, in 4 bits (8 units
+// too) 9.1 / 11.1; 64 of 1024 44.2 / 47.6.  Longer runs of many sequences gain as
+// much where their lengths are equal, but lose more where they are not.
 static int whole_units(int64_t runs) { return runs >= 64 ? 8 : 4; }
 
 // A sequence of the batch as the header reads its arrays.
@@ -168,7 +172,7 @@ __device__ __forceinline__ Found find_unit(const CacheShape& s, const int* lens,
 // ---------------------------------------------------------------------------
 // K and V of a step, from memory to registers
 // ---------------------------------------------------------------------------
-template <typename T, bool FP4, int D> struct KeyStep;
+template <typename T, bool FP4, int D, int TILES> struct KeyStep;
 
 // A load, past the caches or not (see CacheShape::past).
 template <bool PAST, typename V> __device__ __forceinline__ V fetch(const void* p) {
@@ -178,8 +182,8 @@ template <bool PAST, typename V> __device__ __forceinline__ V fetch(const void* 
 
 // The problem's own type.  Chunk i of a key is its values 16 B of which lane
 // group g holds: for bf16 8 values 32 i + 8 g, for fp32 4 values 16 i + 4 g.
-template <typename T, int D> struct KeyStep<T, false, D> {
-    static constexpr int KT = key_tiles(false, sizeof(T), D), N = 16 / sizeof(T);
+template <typename T, int D, int TILES> struct KeyStep<T, false, D, TILES> {
+    static constexpr int KT = TILES, N = 16 / sizeof(T);
     static constexpr int KC = D / 4 / N;              // 16-byte pieces of a key for a lane
     static constexpr int VW = D / 16 * sizeof(T) / 4; // words of a value row for a lane
     u32x4 k[KT][KC];
@@ -227,13 +231,13 @@ template <typename T, int D> struct KeyStep<T, false, D> {
 
 // 4 bits.  A lane holds the D/4 values (D/4) g .. of each of its keys, D/16 of
 // each of its values, and their scales.
-template <typename T, int D> struct KeyStep<T, true, D> {
-    static constexpr int KT = key_tiles(true, sizeof(T), D);
+template <typename T, int D, int TILES> struct KeyStep<T, true, D, TILES> {
+    static constexpr int KT = TILES;
     static constexpr int KC = D / 32;   // words of a key for a lane
     uint32_t k[KT][KC];
     uint32_t ks;        // scales of the lane's KT keys, a byte each
     uint32_t v[4 * KT]; // D = 64: the low half
-    u32x4 vs;           // scales of the lane's 16 values
+    uint32_t vs[KT];    // scales of the lane's 4 KT values
 
     template <bool PAST>
     __device__ __forceinline__ void load(const CacheShape& s, const PagePtrs& pg, int kpage,
@@ -254,9 +258,12 @@ template <typename T, int D> struct KeyStep<T, true, D> {
                 k[t][1] = w[1];
             }
         }
-        ks = fetch<PAST, uint32_t>(
-            (const uint8_t*)pg.ks +
-            ((kh * (D / 32) + g * (D / 4) / 32) << s.page_shift) + (kpos & mask));
+        const uint8_t* ksp = (const uint8_t*)pg.ks +
+                             ((kh * (D / 32) + g * (D / 4) / 32) << s.page_shift) + (kpos & mask);
+        if constexpr (KT == 4)
+            ks = fetch<PAST, uint32_t>(ksp);
+        else
+            ks = fetch<PAST, uint16_t>(ksp);
         const uint8_t* vp = (const uint8_t*)pg.v +
                             ((vh << s.page_shift) + (vpos & mask)) * (D / 2) + D / 32 * m;
 #pragma unroll
@@ -266,14 +273,22 @@ template <typename T, int D> struct KeyStep<T, true, D> {
             else
                 v[x] = fetch<PAST, uint16_t>(vp + x * (D / 2));
         }
-        vs = fetch<PAST, u32x4>(
-            (const uint8_t*)pg.vs +
-            ((vh * (D / 32) + m * (D / 16) / 32) << s.page_shift) + (vpos & mask));
+        const uint8_t* vsp = (const uint8_t*)pg.vs +
+                             ((vh * (D / 32) + m * (D / 16) / 32) << s.page_shift) + (vpos & mask);
+        if constexpr (KT == 4) {
+            const u32x4 w = fetch<PAST, u32x4>(vsp);
+#pragma unroll
+            for (int j = 0; j < KT; ++j) vs[j] = w[j];
+        } else {
+            const u32x2 w = fetch<PAST, u32x2>(vsp);
+            vs[0] = w[0];
+            vs[1] = w[1];
+        }
     }
     // A scale of an unwritten slot may be no number; 0 times a value is 0.
     __device__ __forceinline__ void drop_values(int from) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < KT; ++j) {
             const int keep = min(max(from - 4 * j, 0), 4);
             vs[j] = keep == 4 ? vs[j] : vs[j] & ((1u << (8 * keep)) - 1u);
         }
@@ -402,7 +417,7 @@ template <typename T, bool FP4, int D, int NR> struct Queries {
 // with 64 rows 75 -> 67).  fp32 rows take three terms of the queries and of the
 // probabilities: exact products as with fp32 MFMAs, in a fifth of their cycles.
 template <typename T, bool FP4, int D, int NR> struct Rows {
-    typedef KeyStep<T, FP4, D> Keys;
+    typedef KeyStep<T, FP4, D, key_tiles(FP4, sizeof(T), D, NR)> Keys;
     typedef Queries<T, FP4, D, NR> Q;
     static constexpr int KT = Keys::KT, QC = D / 32, OC = D / 16;
     static constexpr int PT = Q::TERMS == 3 ? 3 : FP4 && NR > 1 ? 1 : 2;   // terms of a probability
@@ -501,7 +516,7 @@ template <typename T, bool FP4, int D, int NR> struct Rows {
 // fp32 products are.  Their rate, 1/16 of bf16's, still outruns the cache's bytes
 // four times.
 template <int D, int NR> struct Rows<float, false, D, NR> {
-    typedef KeyStep<float, false, D> Keys;
+    typedef KeyStep<float, false, D, key_tiles(false, 4, D, NR)> Keys;
     static constexpr int KT = Keys::KT, QC = D / 16, OC = D / 16;
     Queries<float, false, D, NR> q;
     f32x4 o[NR][OC];
@@ -570,7 +585,7 @@ __global__ __launch_bounds__(kAttnThreads, groups_per_cu(FP4, sizeof(T), D, NR))
 cache_attn_kernel(
     CacheShape s, const T* qp, const int* table, const int* lens, const int* starts, PagePtrs pg,
     T* out, float* lse, int max_tiles, int* plan, float2* stat, float* part) {
-    typedef KeyStep<T, FP4, D> Keys;
+    typedef typename Rows<T, FP4, D, NR>::Keys Keys;
     constexpr int KT = Keys::KT, SK = 16 * KT, UNIT = 4 * SK, ROWS = 16 * NR, OC = D / 16;
     constexpr int START = start_units(FP4, NR);
     constexpr int LINE = D + 4;   // a row's outputs in LDS, padded by a bank group
@@ -923,7 +938,7 @@ bool cache_ws(const CacheShape& s, CacheWs* w) {
     const int64_t rows = (int64_t)s.rep * s.max_new;
     const int esz = s.dtype == PROXYATTN_BF16 ? 2 : 4;
     w->tiles = row_tiles(rows, s.fp4, esz);
-    const int unit = 64 * key_tiles(s.fp4, esz, s.d);
+    const int unit = 64 * key_tiles(s.fp4, esz, s.d, w->tiles);
     const int64_t units = (s.max_len + unit - 1) / unit, flat = units + start_units(s.fp4, w->tiles);
     const int64_t runs = (int64_t)s.b * s.hkv * max_row_tiles(s, w->tiles);
     // a workgroup of 256 threads to each run in the second launch
@@ -964,7 +979,7 @@ static void attention_as(const CacheShape& s, const void* q, const int* table, c
         cache_attn_kernel<T, FP4, D, NR, false><<<w.groups, kAttnThreads, 0, st>>>(
             s, (const T*)q, table, lens, starts, pg, (T*)out, lse, mt, plan, stat, part);
     if (!w.joined) return;
-    constexpr int UNIT = 64 * key_tiles(FP4, sizeof(T), D);
+    constexpr int UNIT = 64 * key_tiles(FP4, sizeof(T), D, NR);
     const int rows = std::min(16 * NR, s.rep * s.max_new);
     const unsigned runs = (unsigned)s.b * s.hkv * mt;
     if ((int64_t)runs * rows > kJoinWaves)

@@ -110,12 +110,12 @@ def _call(lib, name, *args):
 
 
 @pytest.mark.parametrize("kw,rows,groups", [
-    # 4 sequences x 8 heads, each 8 units of 128 keys and one for its start (4 bits: two)
+    # 4 sequences x 8 heads, each 8 units of 128 keys and one for its start
     ({}, 16, 288),
-    # 4 bits: units of 256 keys; 8 new tokens of 4 heads
+    # 4 bits, 8 new tokens of 4 heads: 8 units of 256 keys and two
     (dict(cache_type="fp4", max_new=8, num_tokens=32, table_width=32, max_len=2000), 32, 320),
     # at most 4 units, or 8 of 64 runs: a workgroup to each run, no workspace
-    (dict(cache_type="fp4"), 0, 0), (dict(num_seqs=8, num_tokens=8), 0, 0),
+    (dict(cache_type="fp4", max_len=512), 0, 0), (dict(num_seqs=8, num_tokens=8), 0, 0),
     # as many workgroups as two on each of 256 CUs, or one where the rows need the registers
     (dict(num_seqs=64, num_tokens=64, max_len=1025, table_width=17), 16, 512),
     (dict(num_seqs=64, num_tokens=2000, max_new=100, max_len=1025, table_width=17), 64, 256),

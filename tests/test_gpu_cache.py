@@ -670,7 +670,7 @@ def test_shared_pages(pa):
     w.check(q, *w.attend(q), keys, values)
 
 
-@pytest.mark.parametrize("long", [700, 3000])
+@pytest.mark.parametrize("long", [400, 3000])
 def test_step_captured_and_replayed(pa, long):
     """A decode step in a HIP graph, replayed while the lengths grow, each replay
     against the eager step; two captured steps share a workspace.  Runs of a
