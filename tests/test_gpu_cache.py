@@ -472,6 +472,22 @@ def test_attention_of_many_sequences(pa, cache):
     w.check(q, *w.attend(q), keys, values)
 
 
+@pytest.mark.parametrize("b", [2, 63, 64, 65, 256, 257, 700])
+def test_runs_dealt_over_any_number_of_sequences(pa, b):
+    """A few long sequences among short and empty ones: the runs are cut, and every
+    way of finding a workgroup's first one is taken."""
+    rng = np.random.default_rng(b)
+    lens = rng.integers(0, 40, b)
+    lens[[b // 2, b - 1]] = 1500, 2100
+    new = np.minimum(lens, rng.integers(0, 3, b))
+    new[[b // 2, b - 1]] = 1, 2
+    w = Batch(pa, rng, lens.tolist(), new.tolist(), 4, 2, 64, 32, "bf16", "same")
+    assert pa.proxyattn_cache_workspace_size(w.cache) > 0
+    keys, values = w.fill(rng)
+    q = _rand(rng, (w.cache.num_tokens, 4, 64), "bf16")
+    w.check(q, *w.attend(q), keys, values)
+
+
 def test_most_sequences(pa):
     """4096 sequences, most with a token, two long ones: the runs are dealt over
     sequences that nobody keeps at hand."""
