@@ -851,9 +851,13 @@ class Buffers:
 
 
 def prefill(prob: Problem, q, k, v, gamma: float, min_budget_tokens: int = 0,
-            bufs: Buffers | None = None, stream=None) -> Buffers:
-    """Run the three steps (estimate, select_budget, block_sparse_prefill)."""
+            bufs: Buffers | None = None, stream=None, rotary: Rotary | None = None) -> Buffers:
+    """Run the three steps (estimate, select_budget, block_sparse_prefill).  With a
+    rotary, q and k are projections of tokens 0, 1, ..: they are normed and rotated
+    in place first (its output strides have to be the problem's)."""
     bufs = bufs or Buffers(prob, q.device)
+    if rotary is not None:
+        proxyattn_norm_rotate(prob, rotary, q, k, None, 0, q, k, stream)
     proxyattn_estimate(prob, q, k, bufs.logscore, bufs.mass, bufs.workspace, stream)
     proxyattn_select_budget(prob, bufs.logscore, bufs.mass, gamma, min_budget_tokens,
                             bufs.head_count, bufs.block_count, bufs.block_index, stream)

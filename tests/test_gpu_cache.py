@@ -759,6 +759,22 @@ def test_other_stream(pa):
     assert torch.equal(out, want)
 
 
+def test_prefill_with_rotary(pa):
+    """The whole sparse path on projections: the same as on q and k rotated before."""
+    rng = np.random.default_rng(19)
+    n, hq, hkv, d = 1000, 8, 2, 128
+    r = _rotary(pa, rng, d, 128, False, True, "bf16", n)
+    q, k, v = (_rand(rng, (n, h, d), "bf16") for h in (hq, hkv, hkv))
+    prob = pa.Problem(n, hq, hkv, d, 64, 2)
+    qr, kr = torch.empty_like(q), torch.empty_like(k)
+    pa.proxyattn_norm_rotate(prob, r, q, k, None, 0, qr, kr)
+    want = pa.prefill(prob, qr, kr, v, 0.9)
+    got = pa.prefill(prob, q, k, v, 0.9, rotary=r)
+    assert torch.equal(q, qr) and torch.equal(k, kr)
+    for name in ("out", "lse", "logscore", "mass", "head_count", "block_count", "block_index"):
+        assert torch.equal(getattr(got, name), getattr(want, name)), name
+
+
 @pytest.mark.parametrize("cache", ["same", "fp4"])
 def test_prefill_then_decode(pa, cache):
     """A prompt and ten tokens after it as a layer has them: norm and rotation,
