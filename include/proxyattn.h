@@ -444,7 +444,7 @@ int proxyattn_norm_rotate(const proxyattn_problem* p, const proxyattn_rotary* r,
  * such a table gives, the slot holds parts of either.
  *
  * Supported: d in {64, 128}; page_size in {16, 32, 64, 128, 256}; B <= 4096;
- * num_tokens <= 2^26; Hq <= 4096, Hq % Hkv == 0; max_len <= table_width * page_size
+ * num_tokens <= 2^25; Hq <= 4096, Hq % Hkv == 0; max_len <= table_width * page_size
  * <= 2^30.
  */
 typedef struct proxyattn_cache {
@@ -504,7 +504,7 @@ int proxyattn_cache_read(const proxyattn_cache* c, const int32_t* page_table,
  * appended before): the token at position p of sequence b sees cached tokens
  * 0 .. p,
  *     out[t][i] = softmax_u(c <q_t, k_u>) v_u,  lse[i][t] = log sum_u exp(c <q_t, k_u>).
- *  q: [T][Hq][d]; out: [T][Hq][d]; the cache's q and o strides.
+ *  q: [T][Hq][d]; out: [T][Hq][d], apart from q; the cache's q and o strides.
  *  lse: [Hq][T] fp32, or NULL.
  *  workspace: at least proxyattn_cache_workspace_size bytes (which may be 0),
  *      16-byte aligned; nothing in it outlasts the call.

@@ -89,8 +89,9 @@ static int resolve_cache(const proxyattn_cache* c, CacheShape* out) {
                     c->num_tokens);
     if (c->num_seqs > kMaxSeqs)
         return fail(PROXYATTN_E_UNSUPPORTED, "num_seqs %d > %d", c->num_seqs, kMaxSeqs);
-    if (c->num_tokens > 1 << 26)   // workgroups of 256 threads to four tokens each
-        return fail(PROXYATTN_E_UNSUPPORTED, "num_tokens %d > 2^26", c->num_tokens);
+    // workgroups of 256 threads to four tokens each: 2^31 threads, and a grid ends below 2^32
+    if (c->num_tokens > 1 << 25)
+        return fail(PROXYATTN_E_UNSUPPORTED, "num_tokens %d > 2^25", c->num_tokens);
     if (c->max_new < 1 || c->max_len < 1 || c->num_pages < 1 || c->table_width < 1)
         return fail(PROXYATTN_E_INVALID,
                     "max_new, max_len, num_pages and table_width must be positive");

@@ -854,7 +854,8 @@ def prefill(prob: Problem, q, k, v, gamma: float, min_budget_tokens: int = 0,
             bufs: Buffers | None = None, stream=None, rotary: Rotary | None = None) -> Buffers:
     """Run the three steps (estimate, select_budget, block_sparse_prefill).  With a
     rotary, q and k are projections of tokens 0, 1, ..: they are normed and rotated
-    in place first (its output strides have to be the problem's)."""
+    in place first (its output strides have to be the problem's), and stay so should a
+    later step refuse its arguments."""
     bufs = bufs or Buffers(prob, q.device)
     if rotary is not None:
         proxyattn_norm_rotate(prob, rotary, q, k, None, 0, q, k, stream)

@@ -64,7 +64,7 @@ def _cache(**kw):
     (dict(o_tok_stride=4), pa.E_UNSUPPORTED), (dict(dtype="fp32", o_tok_stride=4100), None),
     (dict(softmax_scale=1e-40), pa.E_INVALID), (dict(softmax_scale=1.2e-38), None),
     (dict(softmax_scale=-1.0), None), (dict(softmax_scale=float("inf")), pa.E_INVALID),
-    (dict(num_tokens=2 ** 26 + 1), pa.E_UNSUPPORTED), (dict(num_tokens=2 ** 26), None),
+    (dict(num_tokens=2 ** 25 + 1), pa.E_UNSUPPORTED), (dict(num_tokens=2 ** 25), None),
     # more units of work than an int counts
     (dict(num_seqs=4096, num_q_heads=4096, num_kv_heads=4096), pa.E_UNSUPPORTED),
     (dict(max_new=2 ** 31 - 1), pa.E_UNSUPPORTED),
