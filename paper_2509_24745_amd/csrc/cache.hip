@@ -303,10 +303,11 @@ __device__ __forceinline__ Slot find_slot(const CacheShape& s, const int* table,
     return at;
 }
 
-// The workgroup's place in the row of token blocks: each XCD (workgroups go to
-// them in turn) takes a run of blocks, so that the cache lines that neighbouring
-// blocks share, a page's scales above all, pass through one L2 (80K tokens appended in 4
-// bits and read back 432 -> 425 us, 128K read back 142.4 -> 141.2).
+// The workgroup's place in the row of token blocks when reading back: each XCD
+// (workgroups go to them in turn) takes a run of blocks, so that the cache lines that
+// neighbouring blocks share, a page's scales above all, pass through one L2 (80K tokens
+// of 4 bits read back 65 -> 59 us, 128K 142.4 -> 141.2; appending takes the same time
+// either way).
 __device__ __forceinline__ int token_block() {
     const int x = blockIdx.x % kNumXcd, n = gridDim.x / kNumXcd, rest = gridDim.x % kNumXcd;
     return x * n + min(x, rest) + blockIdx.x / kNumXcd;
@@ -376,7 +377,7 @@ __global__ __launch_bounds__(kRowThreads) void cache_append_kernel(
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int in_row = lane % LR, row_in_wave = lane / LR;
     const LaneChunks lc = lane_chunks<D>(r.rot, in_row);
-    const int t0 = token_block() << shift, mask = (1 << shift) - 1;
+    const int t0 = blockIdx.x << shift, mask = (1 << shift) - 1;
     find_slots<true>(slots, s, table, lens, starts, t0, shift);
     const int qrows = a.q ? s.hq << shift : 0, krows = s.hkv << shift;
     const int qu = (qrows + RW - 1) / RW, ku = (krows + RW - 1) / RW;
